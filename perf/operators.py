@@ -127,8 +127,8 @@ def _prepare_adamw(s, gen):
     s.hyper = dict(lr=1e-5, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01)
     s.max_norm = 1.0
     if case["bits"] == 8:
-        s.m, s.m_scale = _encode(m, None)
-        s.v, s.v_scale = _encode(v, torch.full((total,), 32768, device="cuda"))
+        half = torch.full((total,), 32768, device="cuda")
+        (s.m, s.m_scale), (s.v, s.v_scale) = _encode(m, half, True), _encode(v, half, False)
     else:
         s.m, s.v, s.m_scale, s.v_scale = m, v, None, None
     if own:
@@ -187,19 +187,19 @@ def _train(s):
 
 # ---- the optimizer -------------------------------------------------------------------------------------------------------
 # Moments in 8 bits: blocks of 32 elements share a scale byte, the exponent field of the block's largest magnitude as fp32 (at
-# least 1; 255 for a block that is not finite).  The first moment has a sign, four exponent and three mantissa bits, rounded to nearest
-# even; the second five and three, rounded up with the probability of what is cut off (16 random bits per element), and never to 0.
+# least 1; 255 for a block that is not finite).  The first moment has a sign, four exponent and three mantissa bits, the second five and
+# three and never becomes 0; both are rounded up with the probability of what is cut off (16 random bits per element, for both).
 # What is rounded is the moment in fp32, every operation of its update rounded by itself.
-def _encode(x, random16):
+def _encode(x, random16, first):
     mag = x.abs().view(-1, 32)
     field = (mag.amax(1).view(torch.int32) >> 23).clamp(min=1)
-    lift = ((14 if random16 is None else 30) - field).double()[:, None]
+    lift = ((14 if first else 30) - field).double()[:, None]
     bits = (mag.double() * torch.exp2(lift)).to(torch.float32).view(torch.int32)
-    if random16 is None:
-        code = (bits + 0x7FFFF + ((bits >> 20) & 1)) >> 20
+    code = (bits + (random16.view(-1, 32).to(torch.int32) << 4)) >> 20
+    if first:
         code = code | ((x.view(-1, 32) < 0).to(torch.int32) << 7)
     else:
-        code = torch.where(mag > 0, ((bits + (random16.view(-1, 32).to(torch.int32) << 4)) >> 20).clamp(min=1), torch.zeros_like(bits))
+        code = torch.where(mag > 0, code.clamp(min=1), torch.zeros_like(bits))
     return code.to(torch.uint8).view(-1), field.to(torch.uint8)
 
 
@@ -250,8 +250,8 @@ def _adamw(s):
     s.p.copy_(s.p * (1.0 - h["lr"] * h["weight_decay"]) - (h["lr"] / (1.0 - h["beta1"] ** s.step)) * m / root)
     s.copy.copy_(s.p)
     if case["bits"] == 8:
-        s.m, s.m_scale = _encode(m, None)
-        s.v, s.v_scale = _encode(v, _random16(s.total, s.step, s.seed))
+        random16 = _random16(s.total, s.step, s.seed)
+        (s.m, s.m_scale), (s.v, s.v_scale) = _encode(m, random16, True), _encode(v, random16, False)
         m, v = _decode(s.m, s.m_scale, True), _decode(s.v, s.v_scale, False)
     else:
         s.m.copy_(m)
@@ -328,10 +328,11 @@ def _exact_adamw(s):
     p = s.p.double()
     p = p - h["lr"] * h["weight_decay"] * p - h["lr"] * (m / (1 - h["beta1"] ** t)) / (torch.sqrt(v / (1 - h["beta2"] ** t)) + h["eps"])
     if eight:
+        fraction = torch.from_numpy(_uniform(s.total, t, s.seed)).cuda()
         step = grid(m, 13)
-        m = torch.round(m / step) * step
+        m = torch.floor(m.abs() / step + fraction) * step * torch.sign(m)
         step = grid(v, 29)
-        up = torch.floor(v / step + torch.from_numpy(_uniform(s.total, t, s.seed)).cuda())
+        up = torch.floor(v / step + fraction)
         v = torch.where(v > 0, up.clamp(min=1) * step, torch.zeros_like(v))
     return [p, p, m, v] + ([norm] if s.case["clip"] else [])
 
