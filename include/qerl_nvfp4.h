@@ -527,6 +527,113 @@ QERL_API int mxfp4_lora_linear_native(const void* x_bf16, int64_t M, int64_t K, 
                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * lm_head_logprob* -- log-probability of one token per row under the language-model head, log-sum-exp, entropy, and the
+ * gradient with respect to the hidden states, without keeping the logits.  What a policy update needs above its last
+ * linear: the rollout's and the reference's log-probabilities, the policy's with their gradient, and the entropy that
+ * the paper follows as a measure of exploration (Section 3.3).  With z_v = inv_temperature * x_m . W_v and t the token:
+ *     logprob = z_t - lse,   lse = ln sum_v e^(z_v),   entropy = lse - sum_v p_v z_v,   p_v = e^(z_v - lse)
+ *     slope   = d logprob / dx = inv_temperature * ( (1 - p_t) W_t - sum_{v != t} p_v W_v )
+ * The head is frozen, as all base weights are.  slope is formed beside the log-probabilities, in one pass over pieces of
+ * the vocabulary; a loss then reaches x by lm_head_logprob_backward, dx = bf16(grad_logprob[m] * slope[m]).
+ * Sums are fp32, logits the fp32 sums of exact products, logprob = -ln(1 + sum_{v != t} e^(z_v - z_t)), so that it and
+ * 1 - p_t keep their relative precision where p_t is near 1; in the sum over v the probabilities enter as bf16 (2^-9
+ * relative each).  Results are bit-identical from call to call.
+ *   x [M, ldx], W [V, ldw] bf16, 16-byte aligned, ld % 8 == 0; H % 8 == 0
+ *   Wt: lm_head_prepack_t's output for W (the gradient contracts over the vocabulary; written once, as the weights are frozen)
+ *   targets int64 [M].  A target below 0 marks a row without a loss: its logprob, lse, entropy and slope are 0.  One of V or
+ *     more makes them NaN.
+ *   logprob, lse, entropy fp32 [M] (lse and entropy may be NULL); slope fp32 [M, ld_slope], 16-byte aligned, ld_slope % 4 == 0
+ *   A logit that is not finite leaves the results of its row unspecified (NaN or infinite); other rows are as without it.
+ *   workspace: >= lm_head_logprob_workspace_bytes(M, V, H, gradient) bytes (0 for sizes outside the ranges below), 256-byte
+ *     aligned; needs no initialisation.  Calls that share one must be ordered on one stream.
+ * lm_head_logprob_backward: grad_logprob fp32 [M], dx bf16 [M, lddx], 16-byte aligned, lddx % 8 == 0.
+ * lm_head_prepack_t: Wt [H, V rounded up to 64] bf16, zeros behind V; lm_head_prepack_t_bytes(V, H) bytes, 16-byte aligned.
+ * M == 0 is a no-op.  Errors: NULL pointers; M < 0, V < 1, H < 8, H % 8 != 0, H > 65535 * 64, M or V above 2^31 - 1, a leading dimension
+ * below its row, inv_temperature not positive and finite (QERL_ERR_SHAPE); alignment; workspace.
+ */
+QERL_API size_t lm_head_prepack_t_bytes(int64_t V, int64_t H);   /* host */
+QERL_API int lm_head_prepack_t(const void* W_bf16, int64_t V, int64_t H, int64_t ldw, void* Wt_bf16, void* stream);
+QERL_API size_t lm_head_logprob_workspace_bytes(int64_t M, int64_t V, int64_t H, int gradient);   /* host */
+QERL_API int lm_head_logprob(const void* x_bf16, int64_t M, int64_t H, int64_t ldx, const void* W_bf16, int64_t V, int64_t ldw,
+                             const int64_t* targets, float inv_temperature, float* logprob_f32, float* lse_f32, float* entropy_f32,
+                             void* workspace, size_t workspace_bytes, void* stream);
+QERL_API int lm_head_logprob_grad(const void* x_bf16, int64_t M, int64_t H, int64_t ldx, const void* W_bf16, int64_t V, int64_t ldw,
+                                  const void* Wt_bf16, const int64_t* targets, float inv_temperature, float* logprob_f32,
+                                  float* lse_f32, float* entropy_f32, float* slope_f32, int64_t ld_slope,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+QERL_API int lm_head_logprob_backward(const float* grad_logprob_f32, const float* slope_f32, int64_t ld_slope, int64_t M, int64_t H,
+                                      void* dx_bf16, int64_t lddx, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * lora_adamw_* -- the optimizer step on the adapters (the paper trains A and B with AdamW, moments in 8 bits), all tensors
+ * in one launch.  The gradients are dA_f32 and dB_f32 of the backward functions; the fp32 parameters are the master
+ * values, and each step writes their bf16 copies, the A and B that the linears read.  With g the gradient times
+ * *grad_scale (if given) and t the step:
+ *     m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
+ *     p' = p (1 - lr wd) - lr / (1 - b1^t) m' / ( sqrt(v') / sqrt(1 - b2^t) + eps )
+ * every operation one fp32 rounding, in this order (factors such as lr / (1 - b1^t) are formed in fp64 and rounded once).
+ *
+ * lora_adamw_make_plan writes a table of the tensors into `table` (device memory of lora_adamw_plan_bytes() bytes, 256-byte
+ *   aligned) and fills *plan, a HOST struct that the other calls take.  The table holds the tensors' addresses: the
+ *   gradients of every step are read from grad_f32.  `tensors` is a HOST array, read during the call only.
+ * State: lora_adamw_state_elements() elements; every tensor starts at the next multiple of 32 elements behind the one
+ *   before, what lies between is kept zero.  bits = 32: m and v are fp32.  bits = 8: m and v are bytes, m_scale and
+ *   v_scale one byte per 32 elements, the exponent field f of the block's largest magnitude as fp32 (at least 1; 255 for a
+ *   block with an infinity or a NaN, which reads as NaN throughout).  A byte of m is sign, 4 exponent and 3 mantissa bits e, q
+ *   with the value (8 + q) 2^(e - 14 - 3) 2^(f - 127) (e = 0: q 2^(1 - 14 - 3) 2^(f - 127)); a byte of v 5 and 3 bits, 30 in
+ *   place of 14, and never 0 for a v above zero.  Both are rounded up in magnitude with the probability of what is cut off
+ *   (to nearest, 0.1 and 0.001 of a moment would not move it), by 16 random bits per element:
+ *   Philox4x32 with 10 rounds, counter (b lo, b hi, t lo, t hi), key (seed lo, seed hi), b the group of eight state elements,
+ *   element j of it the low (even j) or high half of word j / 2.  Zero-filled memory is the state before the first step.
+ * lora_adamw_step: one step.  hyper is a HOST struct.  lr_device, step_device and grad_scale are device pointers or NULL:
+ *   *lr_device and *step_device, where given, are read in place of lr and step when the launch runs, so that a captured
+ *   step can be replayed with another rate and step count.  If *grad_scale is not finite the step changes nothing.
+ * lora_adamw_grad_norm: *norm = sqrt(sum g^2) over all gradients, summed in fp64 in a fixed order, and
+ *   *scale = min(1, max_norm / (norm + 1e-6)), NaN if the norm is not finite: pass it as grad_scale.  norm may be NULL.
+ *   workspace: lora_adamw_grad_norm_workspace_bytes() bytes, 256-byte aligned; needs no initialisation.
+ * lora_adamw_moments: the values of an 8-bit state as fp32, m and v [state elements] (inspection, checkpoints).
+ * Errors: NULL pointers (copy_bf16 may be NULL); n < 0, n_tensors outside 1..2^20, more than 2^31 - 1 pieces of 2048
+ * elements, memory that a step writes named twice, bits other than 8 and 32, step < 1, lr, weight_decay < 0 or not
+ * finite, betas outside [0, 1), eps <= 0 (QERL_ERR_SHAPE); parameters, gradients, copies, m or v not 16-byte aligned
+ * (QERL_ERR_ALIGN); table or workspace too small or misaligned (QERL_ERR_WORKSPACE).
+ */
+typedef struct {
+  float* param_f32;            /* [n] updated in place */
+  void* copy_bf16;             /* [n] written by each step, or NULL */
+  const float* grad_f32;       /* [n] */
+  int64_t n;
+} qerl_adamw_tensor;
+typedef struct {
+  const void* table;           /* device */
+  int64_t elements, chunks;
+  int32_t n_tensors;
+} qerl_adamw_plan;
+typedef struct {
+  int32_t bits;                /* 8 or 32 */
+  void* m;
+  void* v;
+  uint8_t* m_scale;            /* bits == 8 only */
+  uint8_t* v_scale;
+} qerl_adamw_state;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;                /* 1 for the first step */
+  uint64_t seed;               /* of the stochastic rounding (bits == 8) */
+  const float* lr_device;
+  const int64_t* step_device;
+  const float* grad_scale;
+} qerl_adamw_hyper;
+QERL_API size_t lora_adamw_plan_bytes(const qerl_adamw_tensor* tensors, int n_tensors);            /* host; 0 for a bad list */
+QERL_API int64_t lora_adamw_state_elements(const qerl_adamw_tensor* tensors, int n_tensors);       /* host; -1 for a bad list */
+QERL_API int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tensors, void* table, size_t table_bytes,
+                                  qerl_adamw_plan* plan, void* stream);
+QERL_API int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_state* state, const qerl_adamw_hyper* hyper, void* stream);
+QERL_API size_t lora_adamw_grad_norm_workspace_bytes(void);                                         /* host */
+QERL_API int lora_adamw_grad_norm(const qerl_adamw_plan* plan, double max_norm, float* norm_f32, float* scale_f32,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+QERL_API int lora_adamw_moments(const qerl_adamw_plan* plan, const qerl_adamw_state* state, float* m_f32, float* v_f32, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement aids: what a kernel on this GPU can reach of the two rooflines the
  * linear is measured against (reported by the benchmark beside the published
  * peaks; no part of the method).

@@ -76,6 +76,21 @@ _SIGNATURES = {
     "aqn_rmsnorm_nvfp4_lora_mlp_workspace_bytes": (_c_sz, [_c_i64] * 7),
     "aqn_rmsnorm_nvfp4_lora_mlp": (ctypes.c_int, [_c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_float,
                                                   _c_p, _c_p, _c_p, _c_p, _c_sz, _c_p]),
+    "lm_head_prepack_t_bytes": (_c_sz, [_c_i64, _c_i64]),
+    "lm_head_prepack_t": (ctypes.c_int, [_c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p]),
+    "lm_head_logprob_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i64, ctypes.c_int]),
+    "lm_head_logprob": (ctypes.c_int, [_c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_i64, _c_i64, _c_p, ctypes.c_float, _c_p, _c_p, _c_p,
+                                       _c_p, _c_sz, _c_p]),
+    "lm_head_logprob_grad": (ctypes.c_int, [_c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_float, _c_p, _c_p,
+                                            _c_p, _c_p, _c_i64, _c_p, _c_sz, _c_p]),
+    "lm_head_logprob_backward": (ctypes.c_int, [_c_p, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_i64, _c_p]),
+    "lora_adamw_plan_bytes": (_c_sz, [_c_p, ctypes.c_int]),
+    "lora_adamw_state_elements": (_c_i64, [_c_p, ctypes.c_int]),
+    "lora_adamw_make_plan": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_sz, _c_p, _c_p]),
+    "lora_adamw_step": (ctypes.c_int, [_c_p, _c_p, _c_p, _c_p]),
+    "lora_adamw_grad_norm_workspace_bytes": (_c_sz, []),
+    "lora_adamw_grad_norm": (ctypes.c_int, [_c_p, ctypes.c_double, _c_p, _c_p, _c_p, _c_sz, _c_p]),
+    "lora_adamw_moments": (ctypes.c_int, [_c_p, _c_p, _c_p, _c_p, _c_p]),
     "qerl_workspace_status": (ctypes.c_int, [_c_p, _c_p]),
     "qerl_status_from_error_word": (ctypes.c_int, [ctypes.c_uint32]),
     "qerl_selftest_wait_gives_up": (ctypes.c_int, [_c_p, ctypes.c_size_t, ctypes.c_uint32, _c_p]),
@@ -137,6 +152,19 @@ def _rows(t: torch.Tensor, name: str):
 
 def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
+
+
+def _here(device, name: str) -> None:
+    """Launches go to the current device's current stream: tensors of another device are refused."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _flat(t: torch.Tensor, dtype, n: int, device, name: str) -> int:
+    p = _dev(t, dtype, name)
+    if not t.is_contiguous() or t.numel() != n or t.device != device:
+        raise ValueError(f"{name} must be contiguous, of {n} elements, on {device}")
+    return p
 
 
 class Workspace:
@@ -403,10 +431,20 @@ def nvfp4_prepack_t(codes: torch.Tensor, scales: torch.Tensor, tensor_scale: tor
     return PackedWeightT(packed, tensor_scale, N, K)
 
 
+def _grad_buffer(t: Optional[torch.Tensor], shape, device, name: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=torch.float32, device=device)
+    if tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be contiguous {list(shape)} on {device}")
+    return t
+
+
 def nvfp4_lora_linear_backward(x, dy, w: PackedWeightT, A: Optional[torch.Tensor] = None,
                                B: Optional[torch.Tensor] = None, lora_scale: float = 0.0,
-                               workspace: Optional[torch.Tensor] = None):
-    """(dx bf16 [M, K], dA fp32 [r, K] or None, dB fp32 [N, r] or None)."""
+                               workspace: Optional[torch.Tensor] = None, dA: Optional[torch.Tensor] = None,
+                               dB: Optional[torch.Tensor] = None):
+    """(dx bf16 [M, K], dA fp32 [r, K] or None, dB fp32 [N, r] or None).  dA, dB: where to write the gradients (an optimizer's
+    buffers), or None for new tensors."""
     lib = load_library()
     M, N, lddy = _rows(dy, "dy")
     K = w.K
@@ -415,7 +453,6 @@ def nvfp4_lora_linear_backward(x, dy, w: PackedWeightT, A: Optional[torch.Tensor
     r = 0
     x_ptr = a_ptr = b_ptr = da_ptr = db_ptr = None
     ldx = K
-    dA = dB = None
     if A is not None and B is not None and A.shape[0] > 0:
         r = A.shape[0]
         if tuple(A.shape) != (r, K) or tuple(B.shape) != (N, r) or not A.is_contiguous() or not B.is_contiguous():
@@ -425,9 +462,10 @@ def nvfp4_lora_linear_backward(x, dy, w: PackedWeightT, A: Optional[torch.Tensor
             raise ValueError("x must be [M, K]")
         x_ptr = _dev(x, torch.bfloat16, "x")
         a_ptr, b_ptr = _dev(A, torch.bfloat16, "A"), _dev(B, torch.bfloat16, "B")
-        dA = torch.empty((r, K), dtype=torch.float32, device=dy.device)
-        dB = torch.empty((N, r), dtype=torch.float32, device=dy.device)
+        dA, dB = _grad_buffer(dA, (r, K), dy.device, "dA"), _grad_buffer(dB, (N, r), dy.device, "dB")
         da_ptr, db_ptr = _dev(dA, torch.float32, "dA"), _dev(dB, torch.float32, "dB")
+    elif dA is not None or dB is not None:
+        raise ValueError("dA and dB belong to an adapter")
     dx = torch.empty((M, K), dtype=torch.bfloat16, device=dy.device)
     need = lib.nvfp4_lora_linear_backward_workspace_bytes(M, N, K, r)
     if workspace is None:
@@ -447,8 +485,10 @@ class _BackwardDesc(ctypes.Structure):
                 ("r", _c_i64), ("lora_scale", ctypes.c_float), ("dA", _c_p), ("dB", _c_p)]
 
 
-def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_scales=None, workspace: Optional[torch.Tensor] = None):
-    """Backward of several linears that read the same x: (dx bf16 [M, K] summed over the members, [(dA_i, dB_i)])."""
+def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_scales=None, workspace: Optional[torch.Tensor] = None,
+                                     dAs=None, dBs=None):
+    """Backward of several linears that read the same x: (dx bf16 [M, K] summed over the members, [(dA_i, dB_i)]).  dAs, dBs: lists of
+    tensors (or None) to write the gradients to."""
     lib = load_library()
     n = len(weights)
     As = As if As is not None else [None] * n
@@ -470,8 +510,8 @@ def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_sca
             r = A.shape[0]
             if tuple(A.shape) != (r, K) or tuple(B.shape) != (N, r) or not A.is_contiguous() or not B.is_contiguous():
                 raise ValueError("A must be contiguous [r, K] and B contiguous [N, r]")
-            dA = torch.empty((r, K), dtype=torch.float32, device=x.device)
-            dB = torch.empty((N, r), dtype=torch.float32, device=x.device)
+            dA = _grad_buffer(dAs[i] if dAs is not None else None, (r, K), x.device, "dA")
+            dB = _grad_buffer(dBs[i] if dBs is not None else None, (N, r), x.device, "dB")
             d.A, d.B, d.r, d.lora_scale = _dev(A, torch.bfloat16, "A"), _dev(B, torch.bfloat16, "B"), r, float(lora_scales[i])
             d.dA, d.dB = _dev(dA, torch.float32, "dA"), _dev(dB, torch.float32, "dB")
         grads.append((dA, dB))
@@ -782,3 +822,217 @@ def mxfp4_lora_linear_native(x: torch.Tensor, w: MxPackedWeight, A: Optional[tor
         _dev(x, torch.bfloat16, "x"), M, K, ldx, _dev(w.packed, torch.uint8, "packed"), w.N, a_ptr, b_ptr, r,
         float(lora_scale), bias_ptr, _dev(out, torch.bfloat16, "out"), ldy, workspace.ptr, workspace.nbytes, _stream()))
     return out
+
+
+# ---- log-probabilities under the language-model head ----------------------------------------------------
+class LmHead:
+    """The frozen head W [V, H] and, for the gradient, its transposed order (lm_head_prepack_t in the header)."""
+
+    def __init__(self, weight: torch.Tensor, weight_t: Optional[torch.Tensor]):
+        self.weight, self.weight_t = weight, weight_t
+        self.V, self.H = weight.shape
+
+
+def lm_head_prepack(W: torch.Tensor, gradient: bool = True) -> LmHead:
+    """W [V, H] bf16 (rows may be strided) as the log-probability functions take it; gradient=False leaves out the transposed order that
+    lm_head_logprob_grad reads."""
+    lib = load_library()
+    V, H, ldw = _rows(W, "W")
+    w_ptr = _dev(W, torch.bfloat16, "W")
+    _here(W.device, "W")
+    wt = None
+    if gradient:
+        wt = torch.empty((H, -(-V // 64) * 64), dtype=torch.bfloat16, device=W.device)
+        _check("lm_head_prepack_t", lib.lm_head_prepack_t(w_ptr, V, H, ldw, wt.data_ptr(), _stream()))
+    return LmHead(W, wt)
+
+
+def lm_head_workspace(M: int, V: int, H: int, gradient: bool = True, device="cuda") -> torch.Tensor:
+    """Scratch for calls of up to M rows; needs no initialisation."""
+    need = int(load_library().lm_head_logprob_workspace_bytes(M, V, H, int(gradient)))
+    if need == 0:
+        raise ValueError("sizes not supported by lm_head_logprob")
+    return torch.empty((need + 256,), dtype=torch.uint8, device=device)
+
+
+def _head_call(name, x, head, targets, inv_temperature, entropy, workspace, out):
+    lib = load_library()
+    gradient = name == "lm_head_logprob_grad"
+    M, H, ldx = _rows(x, "x")
+    x_ptr = _dev(x, torch.bfloat16, "x")
+    _here(x.device, "x")
+    V, Hw, ldw = _rows(head.weight, "W")
+    if H != Hw:
+        raise ValueError("x must have as many columns as the head")
+    if head.weight.device != x.device:
+        raise ValueError("x and the head must be on one device")
+    if gradient and head.weight_t is None:
+        raise ValueError("the head was packed without its transposed order: lm_head_prepack(W, gradient=True)")
+    if out is None:
+        out = [torch.empty((M,), dtype=torch.float32, device=x.device) for _ in range(3 if entropy else 2)]
+        out += [None] * (3 - len(out)) + ([torch.empty((M, H), dtype=torch.float32, device=x.device)] if gradient else [])
+    if len(out) != (4 if gradient else 3):
+        raise ValueError("out must be (logprob, lse, entropy or None%s)" % (", slope" if gradient else ""))
+    if (out[2] is not None) != bool(entropy):
+        raise ValueError("entropy=True and its place in out go together")
+    rows = [_flat(t, torch.float32, M, x.device, n) if t is not None else None for t, n in zip(out, ("logprob", "lse", "entropy"))]
+    t_ptr = _flat(targets, torch.int64, M, x.device, "targets")
+    extra = []
+    if gradient:
+        Ms, Hs, lds = _rows(out[3], "slope")
+        if (Ms, Hs) != (M, H) or out[3].device != x.device:
+            raise ValueError("slope must be [M, H] beside x")
+        extra = [_dev(out[3], torch.float32, "slope"), lds]
+    if workspace is None:
+        workspace = lm_head_workspace(M, V, H, gradient, x.device)
+    base = workspace.data_ptr()
+    ptr = (base + 255) & ~255
+    _check(name, getattr(lib, name)(
+        x_ptr, M, H, ldx, _dev(head.weight, torch.bfloat16, "W"), V, ldw, *([head.weight_t.data_ptr()] if gradient else []), t_ptr,
+        float(inv_temperature), *rows, *extra, ptr, workspace.numel() - (ptr - base), _stream()))
+    return tuple(out)
+
+
+def lm_head_logprob(x, head: LmHead, targets: torch.Tensor, inv_temperature: float = 1.0, entropy: bool = False,
+                    workspace: Optional[torch.Tensor] = None, out=None):
+    """(logprob, lse, entropy or None), fp32 [M], of the tokens `targets` (int64 [M]) under softmax(inv_temperature * x W^T).  A target
+    below 0 marks a row without a loss (zeros), one beyond the vocabulary gives NaN."""
+    return _head_call("lm_head_logprob", x, head, targets, inv_temperature, entropy, workspace, out)
+
+
+def lm_head_logprob_grad(x, head: LmHead, targets: torch.Tensor, inv_temperature: float = 1.0, entropy: bool = False,
+                         workspace: Optional[torch.Tensor] = None, out=None):
+    """(logprob, lse, entropy or None, slope): lm_head_logprob and slope = d logprob / dx, fp32 [M, H], for
+    lm_head_logprob_backward."""
+    return _head_call("lm_head_logprob_grad", x, head, targets, inv_temperature, entropy, workspace, out)
+
+
+def lm_head_logprob_backward(grad_logprob: torch.Tensor, slope: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dx [M, H] bf16 = grad_logprob[m] * slope[m]."""
+    M, H, lds = _rows(slope, "slope")
+    s_ptr = _dev(slope, torch.float32, "slope")
+    _here(slope.device, "slope")
+    if out is None:
+        out = torch.empty((M, H), dtype=torch.bfloat16, device=slope.device)
+    Mo, Ho, lddx = _rows(out, "out")
+    if (Mo, Ho) != (M, H) or out.device != slope.device:
+        raise ValueError("out must be [M, H] beside slope")
+    _check("lm_head_logprob_backward", load_library().lm_head_logprob_backward(
+        _flat(grad_logprob, torch.float32, M, slope.device, "grad_logprob"), s_ptr, lds, M, H, _dev(out, torch.bfloat16, "out"), lddx, _stream()))
+    return out
+
+
+# ---- AdamW on the adapters ---------------------------------------------------------------------------
+class _AdamWTensor(ctypes.Structure):
+    """Mirror of qerl_adamw_tensor in the header."""
+    _fields_ = [("param", _c_p), ("copy", _c_p), ("grad", _c_p), ("n", _c_i64)]
+
+
+class _AdamWPlanStruct(ctypes.Structure):
+    """Mirror of qerl_adamw_plan in the header."""
+    _fields_ = [("table", _c_p), ("elements", _c_i64), ("chunks", _c_i64), ("n_tensors", ctypes.c_int32)]
+
+
+class _AdamWState(ctypes.Structure):
+    """Mirror of qerl_adamw_state in the header."""
+    _fields_ = [("bits", ctypes.c_int32), ("m", _c_p), ("v", _c_p), ("m_scale", _c_p), ("v_scale", _c_p)]
+
+
+class _AdamWHyper(ctypes.Structure):
+    """Mirror of qerl_adamw_hyper in the header."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", _c_i64), ("seed", ctypes.c_uint64), ("lr_device", _c_p),
+                ("step_device", _c_p), ("grad_scale", _c_p)]
+
+
+class AdamWPlan:
+    """The tensors of an optimizer step (see lora_adamw_make_plan in the header) and its moments.  Holds references to all of
+    them; every step reads the gradients from the tensors given here, so the backward pass has to write those (its `dA` and `dB`
+    arguments, or a copy)."""
+
+    def __init__(self, struct, table, tensors, bits, m, v, m_scale, v_scale):
+        self.struct, self.table, self.tensors, self.bits = struct, table, tensors, bits
+        self.m, self.v, self.m_scale, self.v_scale = m, v, m_scale, v_scale
+        self.elements, self.device = int(struct.elements), table.device
+        self._state = _AdamWState(bits, m.data_ptr(), v.data_ptr(), m_scale.data_ptr() if bits == 8 else None,
+                                  v_scale.data_ptr() if bits == 8 else None)
+
+
+def lora_adamw_plan(params, grads, copies=None, state_bits: int = 8, state=None) -> AdamWPlan:
+    """params, grads: lists of contiguous fp32 tensors; copies: None or a list of bf16 tensors (or None) that each step writes
+    from the updated parameters; state: None (zeros) or the moments to go on from, (m, v, m_scale, v_scale) as uint8 for 8 bits,
+    (m, v) as fp32 for 32, laid out as the header says."""
+    lib = load_library()
+    n = len(params)
+    copies = copies if copies is not None else [None] * n
+    if n == 0 or len(grads) != n or len(copies) != n:
+        raise ValueError("params, grads and copies must be lists of one length, not empty")
+    if state_bits not in (8, 32):
+        raise ValueError("state_bits must be 8 or 32")
+    if not params[0].is_cuda:
+        raise TypeError("param must be a GPU tensor")
+    device = params[0].device
+    _here(device, "param")
+    tensors = (_AdamWTensor * n)()
+    for i, (p, g, c) in enumerate(zip(params, grads, copies)):
+        tensors[i] = _AdamWTensor(_flat(p, torch.float32, p.numel(), device, "param"),
+                                  _flat(c, torch.bfloat16, p.numel(), device, "copy") if c is not None else None,
+                                  _flat(g, torch.float32, p.numel(), device, "grad"), p.numel())
+    arr = ctypes.cast(tensors, _c_p)
+    total, need = int(lib.lora_adamw_state_elements(arr, n)), int(lib.lora_adamw_plan_bytes(arr, n))
+    if total < 0 or need == 0:
+        raise ValueError("too many elements")
+    if state is None:
+        dt = torch.uint8 if state_bits == 8 else torch.float32
+        state = [torch.zeros((k,), dtype=dt, device=device) for k in ([total, total] + ([total // 32] * 2 if state_bits == 8 else []))]
+    if len(state) != (4 if state_bits == 8 else 2):
+        raise ValueError("state must be (m, v, m_scale, v_scale) for 8 bits, (m, v) for 32")
+    for t, k, name in zip(state, (total, total, total // 32, total // 32), ("m", "v", "m_scale", "v_scale")):
+        _flat(t, torch.uint8 if state_bits == 8 else torch.float32, k, device, name)
+    m, v, ms, vs = (*state, None, None)[:4]
+    table = torch.empty((need,), dtype=torch.uint8, device=device)
+    struct = _AdamWPlanStruct()
+    _check("lora_adamw_make_plan", lib.lora_adamw_make_plan(arr, n, table.data_ptr(), table.numel(), ctypes.byref(struct), _stream()))
+    return AdamWPlan(struct, table, (list(params), list(grads), list(copies)), state_bits, m, v, ms, vs)
+
+
+def lora_adamw_step(plan: AdamWPlan, lr: Optional[float] = None, step: Optional[int] = None, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, weight_decay: float = 0.0, seed: int = 0, grad_scale: Optional[torch.Tensor] = None,
+                    lr_device: Optional[torch.Tensor] = None, step_device: Optional[torch.Tensor] = None) -> None:
+    """One AdamW step on everything in `plan`, in place.  step counts from 1.  grad_scale: fp32 tensor of one element (from
+    lora_adamw_grad_norm).  lr_device (fp32) and step_device (int64), tensors of one element, take the place of lr and step in steps
+    that are captured and replayed."""
+    if (lr is None) == (lr_device is None) or (step is None) == (step_device is None):
+        raise ValueError("give lr or lr_device, and step or step_device")
+    _here(plan.device, "the plan")
+    one = lambda t, dt, name: _flat(t, dt, 1, plan.device, name) if t is not None else None
+    h = _AdamWHyper(0.0 if lr is None else float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), 1 if step is None else int(step),
+                    seed & (2 ** 64 - 1), one(lr_device, torch.float32, "lr_device"), one(step_device, torch.int64, "step_device"),
+                    one(grad_scale, torch.float32, "grad_scale"))
+    _check("lora_adamw_step", load_library().lora_adamw_step(ctypes.byref(plan.struct), ctypes.byref(plan._state), ctypes.byref(h), _stream()))
+
+
+def lora_adamw_grad_norm(plan: AdamWPlan, max_norm: float, workspace: Optional[torch.Tensor] = None, out=None):
+    """(norm, scale), fp32 tensors of one element: the 2-norm of all gradients of `plan` and the factor that clips it to max_norm
+    (NaN if the norm is not finite), for lora_adamw_step's grad_scale."""
+    lib = load_library()
+    _here(plan.device, "the plan")
+    need = int(lib.lora_adamw_grad_norm_workspace_bytes())
+    if workspace is None:
+        workspace = torch.empty((need + 256,), dtype=torch.uint8, device=plan.device)
+    norm, scale = out if out is not None else torch.empty((2, 1), dtype=torch.float32, device=plan.device).unbind(0)
+    base = workspace.data_ptr()
+    ptr = (base + 255) & ~255
+    _check("lora_adamw_grad_norm", lib.lora_adamw_grad_norm(
+        ctypes.byref(plan.struct), float(max_norm), _flat(norm, torch.float32, 1, plan.device, "norm"),
+        _flat(scale, torch.float32, 1, plan.device, "scale"), ptr, workspace.numel() - (ptr - base), _stream()))
+    return norm, scale
+
+
+def lora_adamw_moments(plan: AdamWPlan):
+    """(m, v) of an 8-bit plan as fp32 [plan.elements]."""
+    _here(plan.device, "the plan")
+    m, v = (torch.empty((plan.elements,), dtype=torch.float32, device=plan.device) for _ in range(2))
+    _check("lora_adamw_moments", load_library().lora_adamw_moments(
+        ctypes.byref(plan.struct), ctypes.byref(plan._state), m.data_ptr(), v.data_ptr(), _stream()))
+    return m, v

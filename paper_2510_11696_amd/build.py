@@ -19,14 +19,14 @@ if os.environ.get("QERL_BUILD_OBJ_DIR"):
     OBJ_DIR = os.environ["QERL_BUILD_OBJ_DIR"]
 
 # -packed-fp32-ops is switched off for all device code (v_pk_*_f32 are not to
-# be generated); quantize.hip additionally forbids fp contraction so that each
-# fp32 operation of the scale chain is rounded on its own.
+# be generated); quantize.hip, mx.hip and adamw.hip additionally forbid fp contraction so that each
+# fp32 operation of the scale chains and of the moments' update is rounded on its own.
 COMMON = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-fvisibility=hidden",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
 ]
-PER_FILE = {"quantize.hip": ["-ffp-contract=off"], "mx.hip": ["-ffp-contract=off"]}
+PER_FILE = {"quantize.hip": ["-ffp-contract=off"], "mx.hip": ["-ffp-contract=off"], "adamw.hip": ["-ffp-contract=off"]}
 # extra hipcc flags for tuning builds, e.g. QERL_EXTRA_HIPCC_FLAGS="-DQERL_TUNING_HOOKS -DQERL_STREAM_TRACE=1"
 COMMON += os.environ.get("QERL_EXTRA_HIPCC_FLAGS", "").split()
 

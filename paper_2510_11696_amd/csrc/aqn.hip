@@ -15,23 +15,9 @@
 // fp32 throughout; sin and cos take the argument in half-turns (exact range reduction).
 #include <math.h>
 #include "common.hpp"
+#include "philox.hpp"
 
 namespace qerl {
-
-struct Philox4 { uint32_t v[4]; };
-
-__device__ __forceinline__ Philox4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
-  constexpr uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u, W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
-#pragma unroll
-  for (int rnd = 0; rnd < 10; ++rnd) {
-    if (rnd) { k0 += W0; k1 += W1; }
-    const uint32_t hi0 = __umulhi(M0, c0), lo0 = M0 * c0;
-    const uint32_t hi1 = __umulhi(M1, c2), lo1 = M1 * c2;
-    const uint32_t n0 = hi1 ^ c1 ^ k0, n2 = hi0 ^ c3 ^ k1;
-    c0 = n0; c1 = lo1; c2 = n2; c3 = lo0;
-  }
-  return Philox4{{c0, c1, c2, c3}};
-}
 
 __device__ __forceinline__ void box_muller(uint32_t ra, uint32_t rb, float& z0, float& z1) {
   const float u1 = (float)((ra >> 8) + 1u) * 0x1p-24f;

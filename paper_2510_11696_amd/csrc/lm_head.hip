@@ -1,0 +1,424 @@
+// lm_head_logprob*: log-probability of one token per row under the language-model head, entropy, and the gradient with respect to
+// the hidden states, without keeping the logits.
+//
+// With z_v = x . W_v / T, t the row's token, o = sum_{v != t} e^(z_v - z_t):
+//   logprob = -ln(1 + o)                       exact near 0, where z_t - lse would have cancelled
+//   lse     = z_t + ln(1 + o)
+//   entropy = lse - sum_v p_v z_v
+//   d logprob / dx = (1/T) [ (1 - p_t) W_t - sum_{v != t} p_v W_v ],   1 - p_t = o / (1 + o)
+// Everything runs on s = z log2(e) with exp2; logits come from bf16 matrix instructions into fp32, all sums are fp32.
+#include <math.h>
+#include "common.hpp"
+#include "lm_head.hpp"
+
+namespace qerl {
+
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kRaise = 60.f;                  // a logit this far (in powers of two) above the reference raises it
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// (m, s, w) <- both, sums relative to the larger m; an m of -inf goes with sums of 0 (or NaN, which has to stay)
+__device__ __forceinline__ void merge_sums(float& m, float& s, float& w, float m2, float s2, float w2) {
+  const float top = fmaxf(m, m2);
+  const float d1 = m == kNegInf ? 0.f : m - top, d2 = m2 == kNegInf ? 0.f : m2 - top;
+  const float e1 = exp2_fast(d1), e2 = exp2_fast(d2);
+  w = (w + d1 * s) * e1 + (w2 + d2 * s2) * e2;
+  s = s * e1 + s2 * e2;
+  m = top;
+}
+
+// ---- a wave's 64 rows x 32 tokens, contraction split over the four waves of the workgroup -------------------------------
+// lane l of a 32 x 32 tile holds of token l % 32 the rows 8 q + 4 (l / 32) + 0..3 as elements 4 q .. 4 q + 3
+enum { kLogits, kProbs, kSums };
+constexpr int kRowsPerBlock = 64, kTokensPerBlock = 32, kKWaves = 4;
+
+template <int MODE>
+__global__ __launch_bounds__(kKWaves * 64) void head_rows_kernel(const HeadArgs a) {
+  __shared__ float sums[kKWaves - 1][32][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n32 = lane & 31, kg = lane >> 5;
+  const int64_t r0 = (int64_t)blockIdx.x * kRowsPerBlock;
+  const int m0 = blockIdx.y * kTokensPerBlock;
+  if (MODE == kProbs && a.flag && !a.flag[blockIdx.y]) return;
+  const int token = m0 + n32 < a.M ? m0 + n32 : a.M - 1;
+  const int64_t ra = r0 + n32 < a.rows ? r0 + n32 : a.rows - 1, rb = r0 + 32 + n32 < a.rows ? r0 + 32 + n32 : a.rows - 1;
+  const uint16_t* pa = a.a + ra * a.lda;
+  const uint16_t* pb = a.a + rb * a.lda;
+  const uint16_t* px = a.b + (int64_t)token * a.ldb;
+  f32x16 acc[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+  const int64_t steps = (a.k + 15) / 16, part = (int64_t)wave + (MODE == kSums ? (int64_t)blockIdx.z * kKWaves : 0), parts = (int64_t)kKWaves * (MODE == kSums ? a.split : 1);
+  const int64_t s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
+  auto load = [&](const uint16_t* p, int64_t s) {      // k is a multiple of 8: a chunk of eight is inside or beyond
+    const int64_t at = s * 16 + kg * 8;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p + (at < a.k ? at : a.k - 8));
+    return __builtin_bit_cast(bf16x8, at < a.k ? v : u32x4{0u, 0u, 0u, 0u});
+  };
+  for (int64_t s = s0; s < s1; ++s) {
+    const bf16x8 x = load(px, s);
+    acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load(pa, s), x, acc[0], 0, 0, 0);
+    acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load(pb, s), x, acc[1], 0, 0, 0);
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sums[wave - 1][i][lane] = acc[i >> 4][i & 15];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) acc[i >> 4][i & 15] = (acc[i >> 4][i & 15] + sums[0][i][lane]) + (sums[1][i][lane] + sums[2][i][lane]);
+
+  const bool live = m0 + n32 < a.M;
+  if constexpr (MODE == kSums) {
+    if (!live) return;
+    const float alpha = a.first ? 0.f : exp2_fast(a.ref[token] == a.ref_next[token] ? 0.f : a.ref[token] - a.ref_next[token]);
+    float* out = a.acc + (int64_t)blockIdx.z * a.slab + (int64_t)token * a.ld_acc;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int64_t r = r0 + (i >> 4) * 32 + 8 * ((i >> 2) & 3) + 4 * kg + (i & 3);
+      if (r < a.rows) out[r] = a.first ? acc[i >> 4][i & 15] : alpha * out[r] + acc[i >> 4][i & 15];
+    }
+  } else {
+    const int64_t target = a.targets[token] - a.row0;
+    const float ref = MODE == kProbs ? (a.flag ? a.ref_next : a.ref)[token] : 0.f;
+    float top = kNegInf;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int64_t r = r0 + (i >> 4) * 32 + 8 * ((i >> 2) & 3) + 4 * kg + (i & 3);
+      float v = acc[i >> 4][i & 15] * a.scale;
+      if (r == target && live) a.target_logit[token] = v;
+      if (r == target || r >= a.rows) v = kNegInf;
+      acc[i >> 4][i & 15] = v;
+      top = fmaxf(top, v);
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float base = MODE == kProbs ? ref : top == kNegInf ? 0.f : top;
+    float sum = 0.f, weighted = 0.f;
+    uint32_t pr[16];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float d = acc[i >> 4][i & 15] - base, e = exp2_fast(d);
+      sum += e;
+      weighted += d == kNegInf ? 0.f : e * d;
+      if (MODE == kProbs) { if (i & 1) pr[i >> 1] |= f32_to_bf16_bits(e) << 16; else pr[i >> 1] = f32_to_bf16_bits(e); }
+    }
+    sum += __shfl_xor(sum, 32, 64);
+    weighted += __shfl_xor(weighted, 32, 64);
+    if (!live) return;
+    if (kg == 0) a.part[(int64_t)token * a.part_ld + a.block0 + blockIdx.x] = HeadPart{MODE == kProbs ? ref : top, sum, weighted, top};
+    if (MODE == kProbs) {
+      uint16_t* out = a.p + (int64_t)token * a.ldp;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int64_t r = r0 + (q >> 2) * 32 + 8 * (q & 3) + 4 * kg;
+        if (r < a.ldp) *reinterpret_cast<u32x2*>(out + r) = u32x2{pr[2 * q], pr[2 * q + 1]};
+      }
+    }
+  }
+}
+
+// Reference of the first piece: the logit of the row's token (a lower bound of the row's largest); rows without a loss get +inf, which
+// makes their probabilities 0.
+__global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, float* ref) {
+  const int token = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (token >= a.M) return;
+  const int64_t target = a.targets[token];
+  if (target < 0 || target >= a.V) {
+    if (lane == 0) ref[token] = kInf;
+    return;
+  }
+  const uint16_t* x = a.b + (int64_t)token * a.ldb;
+  const uint16_t* w = a.a + target * a.lda;
+  float sum = 0.f;
+  for (int64_t k = lane * 8; k < a.k; k += 512) {
+    const u32x4 xv = *reinterpret_cast<const u32x4*>(x + k), wv = *reinterpret_cast<const u32x4*>(w + k);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum += bf16_bits_to_f32(xv[j] & 0xffffu) * bf16_bits_to_f32(wv[j] & 0xffffu);
+      sum += __uint_as_float(xv[j] & 0xffff0000u) * __uint_as_float(wv[j] & 0xffff0000u);
+    }
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) ref[token] = sum * a.scale;
+}
+
+// After a piece: references of the next one, and which token blocks have to compute the piece again
+__global__ __launch_bounds__(256) void head_check_kernel(const HeadPart* part, int64_t part_ld, int block0, int blocks, int M, int tokens_per_flag,
+                                                         const float* ref, float* ref_next, int* flag) {
+  __shared__ int raised;
+  if (threadIdx.x == 0) raised = 0;
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int i = wave; i < tokens_per_flag; i += 4) {
+    const int token = blockIdx.x * tokens_per_flag + i;
+    if (token >= M) break;
+    float top = kNegInf;
+    for (int b = lane; b < blocks; b += 64) top = fmaxf(top, part[(int64_t)token * part_ld + block0 + b].top);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    const float r = ref[token];
+    const bool up = top > r + kRaise;
+    if (lane == 0) {
+      ref_next[token] = up ? top : r;
+      if (up) raised = 1;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) flag[blockIdx.x] = raised;
+}
+
+// Row results from the parts of all row blocks; for the gradient also 1 - p_t and what turns the sums E into sum p W
+__global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int blocks, const float* ref_last, float* logprob, float* lse, float* entropy,
+                                                          float* rest, float* e_scale) {
+  __shared__ float sm[3][4];
+  const int token = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t target = a.targets[token];
+  if (target < 0 || target >= a.V) {
+    if (threadIdx.x == 0) {
+      const float v = target < 0 ? 0.f : __uint_as_float(0x7fc00000u);
+      logprob[token] = v;
+      if (lse) lse[token] = v;
+      if (entropy) entropy[token] = v;
+      if (rest) { rest[token] = v; e_scale[token] = 0.f; }
+    }
+    return;
+  }
+  float m = kNegInf, s = 0.f, w = 0.f;
+  for (int b = threadIdx.x; b < blocks; b += 256) {
+    const HeadPart p = a.part[(int64_t)token * a.part_ld + b];
+    merge_sums(m, s, w, p.ref, p.sum, p.weighted);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64), w2 = __shfl_xor(w, o, 64);
+    merge_sums(m, s, w, m2, s2, w2);
+  }
+  if (lane == 0) { sm[0][wave] = m; sm[1][wave] = s; sm[2][wave] = w; }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int i = 1; i < 4; ++i) merge_sums(m, s, w, sm[0][i], sm[1][i], sm[2][i]);
+  const float st = a.target_logit[token];
+  float base, total, logp, l;
+  if (!(st < m - 30.f)) {
+    base = st;                                   // relative to the token itself: nothing cancels
+    const float d = m == kNegInf ? 0.f : m - st, f = exp2_fast(d);
+    w = (w + d * s) * f;
+    s *= f;
+    total = 1.f + s;
+    l = log1pf(s);
+    logp = -l;
+  } else {
+    base = m;
+    const float et = exp2_fast(st - m);
+    total = s + et;
+    w += et * (st - m);
+    l = logf(total);
+    logp = kLn2 * (st - m) - l;
+  }
+  logprob[token] = logp;
+  if (lse) lse[token] = kLn2 * base + l;
+  if (entropy) entropy[token] = l - kLn2 * w / total;
+  if (rest) {
+    rest[token] = s / total;
+    e_scale[token] = exp2_fast(ref_last[token] - base) / total;
+  }
+}
+
+// slope = (1/T) [ (1 - p_t) W_t - sum_{v != t} p_v W_v ]
+__global__ __launch_bounds__(256) void head_slope_kernel(const HeadArgs a, int64_t H, float inv_temperature, const float* rest, const float* e_scale,
+                                                         float* slope, int64_t ld_slope) {
+  const int token = blockIdx.x;
+  const int64_t target = a.targets[token];
+  float* out = slope + (int64_t)token * ld_slope;
+  const float r = rest[token], e = e_scale[token];
+  const bool none = target < 0 || target >= a.V;
+  const uint16_t* w = a.a + (none ? 0 : target) * a.lda;
+  for (int64_t h = threadIdx.x; h < H; h += 256) {
+    if (none) { out[h] = r; continue; }
+    float sum = 0.f;
+    for (int z = 0; z < a.split; ++z) sum += a.acc[z * a.slab + (int64_t)token * a.ld_acc + h];
+    out[h] = inv_temperature * (bf16_bits_to_f32(w[h]) * r - sum * e);
+  }
+}
+
+// dx = bf16(g slope)
+__global__ __launch_bounds__(256) void head_backward_kernel(const float* g, const float* slope, int64_t ld_slope, int M, int64_t H, uint16_t* dx, int64_t lddx) {
+  const int token = blockIdx.y;
+  const int64_t h = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (h >= H) return;
+  const float gm = g[token];
+  const f32x4 a = *reinterpret_cast<const f32x4*>(slope + token * ld_slope + h), b = *reinterpret_cast<const f32x4*>(slope + token * ld_slope + h + 4);
+  *reinterpret_cast<u32x4*>(dx + token * lddx + h) =
+      u32x4{pack_bf16x2(gm * a[0], gm * a[1]), pack_bf16x2(gm * a[2], gm * a[3]), pack_bf16x2(gm * b[0], gm * b[1]), pack_bf16x2(gm * b[2], gm * b[3])};
+}
+
+// W [V, ldw] -> Wt [H, ldt], ldt = V rounded up to 64, zeros behind the vocabulary
+__global__ __launch_bounds__(256) void head_transpose_kernel(const uint16_t* w, int64_t V, int64_t H, int64_t ldw, uint16_t* out, int64_t ldt) {
+  __shared__ uint16_t tile[64][66];
+  const int64_t v0 = (int64_t)blockIdx.x * 64, h0 = (int64_t)blockIdx.y * 64;
+  const int c = threadIdx.x & 63;
+  for (int r = threadIdx.x >> 6; r < 64; r += 4) tile[r][c] = v0 + r < V && h0 + c < H ? w[(v0 + r) * ldw + h0 + c] : 0;
+  __syncthreads();
+  for (int r = threadIdx.x >> 6; r < 64; r += 4)
+    if (h0 + r < H) out[(h0 + r) * ldt + v0 + c] = tile[c][r];
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+constexpr int64_t kMaxHidden = 65535 * 64;
+constexpr int64_t kTokenBlock = 8192;                     // tokens that are taken through the whole vocabulary together
+constexpr int64_t kPieceBytes = (int64_t)192 << 20;       // probabilities of a piece: they stay in the last-level cache until they are used
+
+struct HeadPlan {
+  int64_t tokens, blocks, pieces, piece;                  // tokens at a time; row blocks; pieces and their rows (a multiple of 64)
+  int split;
+  size_t part, target, ref, flag, rest, p, acc, bytes;    // offsets
+};
+static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
+  HeadPlan q = {};
+  q.tokens = M < kTokenBlock ? M : kTokenBlock;
+  q.blocks = ceil_div(V, kRowsPerBlock);
+  q.pieces = 1;
+  q.piece = q.blocks * kRowsPerBlock;
+  q.split = 1;
+  auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
+  size_t at = 0;
+  q.part = at; at += up((size_t)(q.tokens * q.blocks) * sizeof(HeadPart));
+  q.target = at; at += up((size_t)q.tokens * 4);
+  if (gradient) {
+    int64_t rows = kPieceBytes / (2 * q.tokens) / kRowsPerBlock * kRowsPerBlock;
+    rows = rows < kRowsPerBlock ? kRowsPerBlock : rows;
+    q.pieces = ceil_div(q.piece, rows);
+    q.piece = ceil_div(ceil_div(q.piece, q.pieces), kRowsPerBlock) * kRowsPerBlock;
+    q.pieces = ceil_div(V, q.piece);
+    const int64_t groups = ceil_div(H, kRowsPerBlock) * ceil_div(q.tokens, kTokensPerBlock);
+    q.split = (int)(groups >= 512 ? 1 : ceil_div(512, groups));
+    if (q.split > 32) q.split = 32;
+    q.ref = at; at += up((size_t)(q.tokens * (q.pieces + 1)) * 4);
+    q.flag = at; at += up((size_t)ceil_div(q.tokens, kTokensPerBlock) * 4);
+    q.rest = at; at += up((size_t)(2 * q.tokens) * 4);
+    q.p = at; at += up((size_t)(q.tokens * q.piece) * 2);
+    q.acc = at; at += up((size_t)(q.split * q.tokens * H) * 4);
+  }
+  q.bytes = at;
+  return q;
+}
+
+struct HeadCall {
+  const uint16_t* x; int64_t M, H, ldx;
+  const uint16_t* W; int64_t V, ldw;
+  const uint16_t* Wt;
+  const int64_t* targets; float inv_temperature;
+  float* logprob; float* lse; float* entropy; float* slope; int64_t ld_slope;
+  uint8_t* ws; size_t ws_bytes; hipStream_t st;
+};
+
+static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t M) {
+  HeadArgs a = {};
+  a.a = c.W; a.lda = c.ldw; a.rows = c.V; a.b = c.x + m0 * c.ldx; a.ldb = c.ldx; a.k = c.H; a.M = (int)M;
+  a.targets = c.targets + m0; a.V = c.V; a.scale = c.inv_temperature * 1.44269504088896341f;
+  a.part = reinterpret_cast<HeadPart*>(c.ws + q.part); a.part_ld = q.blocks; a.target_logit = reinterpret_cast<float*>(c.ws + q.target);
+  const unsigned tb = (unsigned)ceil_div(M, kTokensPerBlock);
+  float* logprob = c.logprob + m0;
+  float* lse = c.lse ? c.lse + m0 : nullptr;
+  float* entropy = c.entropy ? c.entropy + m0 : nullptr;
+  if (!c.slope) {
+    head_rows_kernel<kLogits><<<dim3((unsigned)q.blocks, tb), dim3(kKWaves * 64), 0, c.st>>>(a);
+    head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.blocks, nullptr, logprob, lse, entropy, nullptr, nullptr);
+    return launch_status();
+  }
+  float* ref = reinterpret_cast<float*>(c.ws + q.ref);
+  int* flag = reinterpret_cast<int*>(c.ws + q.flag);
+  float* rest = reinterpret_cast<float*>(c.ws + q.rest);
+  float* e_scale = rest + q.tokens;
+  const int64_t ldt = ceil_div(c.V, 64) * 64;
+  head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref);
+  HeadArgs e = a;
+  e.lda = ldt; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
+  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.ld_acc = c.H; e.slab = q.tokens * c.H; e.split = q.split;
+  for (int64_t i = 0; i < q.pieces; ++i) {
+    const int64_t row0 = i * q.piece, rows = c.V - row0 < q.piece ? c.V - row0 : q.piece;
+    a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.block0 = (int)(row0 / kRowsPerBlock);
+    a.p = reinterpret_cast<uint16_t*>(c.ws + q.p); a.ldp = q.piece;
+    a.ref = ref + i * q.tokens; a.ref_next = ref + (i + 1) * q.tokens; a.flag = nullptr;
+    const unsigned rb = (unsigned)ceil_div(rows, kRowsPerBlock);
+    head_rows_kernel<kProbs><<<dim3(rb, tb), dim3(kKWaves * 64), 0, c.st>>>(a);
+    head_check_kernel<<<dim3(tb), dim3(256), 0, c.st>>>(a.part, a.part_ld, a.block0, (int)rb, (int)M, kTokensPerBlock, a.ref, ref + (i + 1) * q.tokens, flag);
+    a.flag = flag;
+    head_rows_kernel<kProbs><<<dim3(rb, tb), dim3(kKWaves * 64), 0, c.st>>>(a);
+    e.a = c.Wt + row0; e.k = (int64_t)rb * kRowsPerBlock; e.ref = a.ref; e.ref_next = a.ref_next; e.first = i == 0;
+    head_rows_kernel<kSums><<<dim3((unsigned)ceil_div(c.H, kRowsPerBlock), tb, (unsigned)q.split), dim3(kKWaves * 64), 0, c.st>>>(e);
+  }
+  const float* ref_last = ref + q.pieces * q.tokens;
+  head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.blocks, ref_last, logprob, lse, entropy, rest, e_scale);
+  a.a = c.W; a.acc = e.acc; a.ld_acc = e.ld_acc; a.slab = e.slab; a.split = e.split;
+  head_slope_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, c.H, c.inv_temperature, rest, e_scale, c.slope + m0 * c.ld_slope, c.ld_slope);
+  return launch_status();
+}
+
+static int run_head(const HeadCall& c, bool gradient) {
+  if (c.M < 0 || c.V < 1 || c.V > 0x7fffffff || c.H < 8 || c.H % 8 != 0 || c.H > kMaxHidden || c.M > 0x7fffffff || c.ldx < c.H || c.ldw < c.H || (gradient && c.ld_slope < c.H))
+    return QERL_ERR_SHAPE;
+  if (!(c.inv_temperature > 0.f) || !isfinite(c.inv_temperature)) return QERL_ERR_SHAPE;
+  if (c.M == 0) return QERL_OK;
+  if (!c.x || !c.W || !c.targets || !c.logprob || (gradient && (!c.Wt || !c.slope))) return QERL_ERR_NULL;
+  if (!aligned(c.x, 16) || !aligned(c.W, 16) || !aligned(c.Wt, 16) || !aligned(c.slope, 16) || c.ldx % 8 || c.ldw % 8 || (gradient && c.ld_slope % 4) ||
+      !aligned(c.targets, 8) || !aligned(c.logprob, 4) || !aligned(c.lse, 4) || !aligned(c.entropy, 4))
+    return QERL_ERR_ALIGN;
+  const HeadPlan q = plan_head(c.M, c.V, c.H, gradient);
+  if (!c.ws || !aligned(c.ws, 256) || c.ws_bytes < q.bytes) return QERL_ERR_WORKSPACE;
+  for (int64_t m0 = 0; m0 < c.M; m0 += q.tokens)
+    if (const int e = run_tokens(c, q, m0, c.M - m0 < q.tokens ? c.M - m0 : q.tokens)) return e;
+  return QERL_OK;
+}
+
+}  // namespace qerl
+
+using namespace qerl;
+
+extern "C" size_t lm_head_prepack_t_bytes(int64_t V, int64_t H) {
+  return V < 1 || H < 1 ? 0 : (size_t)(ceil_div(V, 64) * 64) * (size_t)H * 2;
+}
+extern "C" int lm_head_prepack_t(const void* W, int64_t V, int64_t H, int64_t ldw, void* Wt, void* stream) {
+  if (V < 0 || H < 0 || V > 0x7fffffff || H % 8 != 0 || H > kMaxHidden || ldw < H) return QERL_ERR_SHAPE;
+  if (V == 0 || H == 0) return QERL_OK;
+  if (!W || !Wt) return QERL_ERR_NULL;
+  if (!aligned(W, 16) || !aligned(Wt, 16) || ldw % 8) return QERL_ERR_ALIGN;
+  const int64_t vb = ceil_div(V, 64);
+  head_transpose_kernel<<<dim3((unsigned)vb, (unsigned)ceil_div(H, 64)), dim3(256), 0, (hipStream_t)stream>>>(
+      static_cast<const uint16_t*>(W), V, H, ldw, static_cast<uint16_t*>(Wt), vb * 64);
+  return launch_status();
+}
+
+extern "C" size_t lm_head_logprob_workspace_bytes(int64_t M, int64_t V, int64_t H, int gradient) {
+  if (M < 0 || V < 1 || H < 8 || M > 0x7fffffff || V > 0x7fffffff) return 0;
+  return M == 0 ? 256 : plan_head(M, V, H, gradient != 0).bytes;
+}
+
+extern "C" int lm_head_logprob(const void* x, int64_t M, int64_t H, int64_t ldx, const void* W, int64_t V, int64_t ldw, const int64_t* targets,
+                               float inv_temperature, float* logprob, float* lse, float* entropy, void* ws, size_t ws_bytes, void* stream) {
+  return run_head(HeadCall{static_cast<const uint16_t*>(x), M, H, ldx, static_cast<const uint16_t*>(W), V, ldw, nullptr, targets, inv_temperature, logprob, lse,
+                           entropy, nullptr, 0, static_cast<uint8_t*>(ws), ws_bytes, (hipStream_t)stream}, false);
+}
+extern "C" int lm_head_logprob_grad(const void* x, int64_t M, int64_t H, int64_t ldx, const void* W, int64_t V, int64_t ldw, const void* Wt,
+                                    const int64_t* targets, float inv_temperature, float* logprob, float* lse, float* entropy, float* slope,
+                                    int64_t ld_slope, void* ws, size_t ws_bytes, void* stream) {
+  return run_head(HeadCall{static_cast<const uint16_t*>(x), M, H, ldx, static_cast<const uint16_t*>(W), V, ldw, static_cast<const uint16_t*>(Wt), targets,
+                           inv_temperature, logprob, lse, entropy, slope, ld_slope, static_cast<uint8_t*>(ws), ws_bytes, (hipStream_t)stream}, true);
+}
+extern "C" int lm_head_logprob_backward(const float* grad, const float* slope, int64_t ld_slope, int64_t M, int64_t H, void* dx, int64_t lddx, void* stream) {
+  if (M < 0 || M > 0x7fffffff || H < 8 || H % 8 || H > kMaxHidden || ld_slope < H || lddx < H) return QERL_ERR_SHAPE;
+  if (M == 0) return QERL_OK;
+  if (!grad || !slope || !dx) return QERL_ERR_NULL;
+  if (!aligned(grad, 4) || !aligned(slope, 16) || !aligned(dx, 16) || ld_slope % 4 || lddx % 8) return QERL_ERR_ALIGN;
+  for (int64_t m0 = 0; m0 < M; m0 += 65535) {
+    const int n = (int)(M - m0 < 65535 ? M - m0 : 65535);
+    head_backward_kernel<<<dim3((unsigned)ceil_div(H, 2048), (unsigned)n), dim3(256), 0, (hipStream_t)stream>>>(
+        grad + m0, slope + m0 * ld_slope, ld_slope, n, H, static_cast<uint16_t*>(dx) + m0 * lddx, lddx);
+  }
+  return launch_status();
+}
