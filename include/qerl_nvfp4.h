@@ -544,12 +544,12 @@ QERL_API int mxfp4_lora_linear_native(const void* x_bf16, int64_t M, int64_t K, 
  *     more makes them NaN.
  *   logprob, lse, entropy fp32 [M] (lse and entropy may be NULL); slope fp32 [M, ld_slope], 16-byte aligned, ld_slope % 4 == 0
  *   A logit that is not finite leaves the results of its row unspecified (NaN or infinite); other rows are as without it.
- *   workspace: >= lm_head_logprob_workspace_bytes(M, V, H, gradient) bytes (0 for sizes outside the ranges below), 256-byte
- *     aligned; needs no initialisation.  Calls that share one must be ordered on one stream.
+ *   workspace: >= lm_head_logprob_workspace_bytes(M, V, H, gradient) bytes (0 for sizes outside the ranges below; one sized for M
+ *     rows serves fewer as well), 256-byte aligned; needs no initialisation.  Calls that share one must be ordered on one stream.
  * lm_head_logprob_backward: grad_logprob fp32 [M], dx bf16 [M, lddx], 16-byte aligned, lddx % 8 == 0.
  * lm_head_prepack_t: Wt [H, V rounded up to 64] bf16, zeros behind V; lm_head_prepack_t_bytes(V, H) bytes, 16-byte aligned.
- * M == 0 is a no-op.  Errors: NULL pointers; M < 0, V < 1, H < 8, H % 8 != 0, H > 65535 * 64, M or V above 2^31 - 1, a leading dimension
- * below its row, inv_temperature not positive and finite (QERL_ERR_SHAPE); alignment; workspace.
+ * M == 0 is a no-op.  Errors: NULL pointers; M < 0, V < 1, V > 2^22, H < 8, H % 8 != 0, M > 2^31 - 1, a leading dimension below its
+ * row, ldx or ldw >= 2^18, inv_temperature not positive and finite (QERL_ERR_SHAPE); alignment; workspace.
  */
 QERL_API size_t lm_head_prepack_t_bytes(int64_t V, int64_t H);   /* host */
 QERL_API int lm_head_prepack_t(const void* W_bf16, int64_t V, int64_t H, int64_t ldw, void* Wt_bf16, void* stream);

@@ -13,10 +13,7 @@
 
 namespace qerl {
 
-constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kInf = __builtin_huge_valf();
 constexpr float kLn2 = 0.693147180559945309f;
-constexpr float kRaise = 60.f;                  // a logit this far (in powers of two) above the reference raises it
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -32,10 +29,9 @@ __device__ __forceinline__ void merge_sums(float& m, float& s, float& w, float m
 
 // ---- a wave's 64 rows x 32 tokens, contraction split over the four waves of the workgroup -------------------------------
 // lane l of a 32 x 32 tile holds of token l % 32 the rows 8 q + 4 (l / 32) + 0..3 as elements 4 q .. 4 q + 3
-enum { kLogits, kProbs, kSums };
 constexpr int kRowsPerBlock = 64, kTokensPerBlock = 32, kKWaves = 4;
 
-template <int MODE>
+template <HeadMode MODE>
 __global__ __launch_bounds__(kKWaves * 64) void head_rows_kernel(const HeadArgs a) {
   __shared__ float sums[kKWaves - 1][32][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n32 = lane & 31, kg = lane >> 5;
@@ -110,7 +106,7 @@ __global__ __launch_bounds__(kKWaves * 64) void head_rows_kernel(const HeadArgs 
     sum += __shfl_xor(sum, 32, 64);
     weighted += __shfl_xor(weighted, 32, 64);
     if (!live) return;
-    if (kg == 0) a.part[(int64_t)token * a.part_ld + a.block0 + blockIdx.x] = HeadPart{MODE == kProbs ? ref : top, sum, weighted, top};
+    if (kg == 0) a.part[(int64_t)token * a.part_ld + a.part0 + blockIdx.x] = HeadPart{MODE == kProbs ? ref : top, sum, weighted, top};
     if (MODE == kProbs) {
       uint16_t* out = a.p + (int64_t)token * a.ldp;
 #pragma unroll
@@ -122,17 +118,44 @@ __global__ __launch_bounds__(kKWaves * 64) void head_rows_kernel(const HeadArgs 
   }
 }
 
-// Reference of the first piece: the logit of the row's token (a lower bound of the row's largest); rows without a loss get +inf, which
-// makes their probabilities 0.
-__global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, float* ref) {
+// Rows with a loss, in order: index[0 .. *count), and each row's place among them (-1: none)
+constexpr int kCompactThreads = 1024;
+__global__ __launch_bounds__(kCompactThreads) void head_compact_kernel(const int64_t* targets, int64_t V, int M, int* index, int* place, int* count) {
+  __shared__ int waves[kCompactThreads / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int m0 = 0; m0 < M; m0 += kCompactThreads) {
+    const int m = m0 + threadIdx.x;
+    const bool in = m < M && targets[m] >= 0 && targets[m] < V;
+    const uint64_t votes = __ballot(in);
+    if (lane == 0) waves[wave] = __popcll(votes);
+    __syncthreads();
+    int at = before, all = 0;
+    for (int w = 0; w < kCompactThreads / 64; ++w) {
+      if (w < wave) at += waves[w];
+      all += waves[w];
+    }
+    at += __popcll(votes & (((uint64_t)1 << lane) - 1));
+    if (in) index[at] = m;
+    if (m < M) place[m] = in ? at : -1;
+    before += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *count = before;
+}
+
+// Reference of the first piece: the logit of the token's own row (a lower bound of the largest).  A row without a loss, where such are not
+// left out, gets +inf, which makes its probabilities 0.  Clears the pieces' flags.
+__global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, float* ref, int* flags, int n_flags) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n_flags; i += gridDim.x * 256) flags[i] = 0;
   const int token = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (token >= a.M) return;
-  const int64_t target = a.targets[token];
+  if (token >= head_tokens(a)) return;
+  const int64_t row = head_row(a, token), target = a.targets[row];
   if (target < 0 || target >= a.V) {
     if (lane == 0) ref[token] = kInf;
     return;
   }
-  const uint16_t* x = a.b + (int64_t)token * a.ldb;
+  const uint16_t* x = a.b + row * a.ldb;
   const uint16_t* w = a.a + target * a.lda;
   float sum = 0.f;
   for (int64_t k = lane * 8; k < a.k; k += 512) {
@@ -147,49 +170,41 @@ __global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, f
   if (lane == 0) ref[token] = sum * a.scale;
 }
 
-// After a piece: references of the next one, and which token blocks have to compute the piece again
-__global__ __launch_bounds__(256) void head_check_kernel(const HeadPart* part, int64_t part_ld, int block0, int blocks, int M, int tokens_per_flag,
-                                                         const float* ref, float* ref_next, int* flag) {
-  __shared__ int raised;
-  if (threadIdx.x == 0) raised = 0;
-  __syncthreads();
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = wave; i < tokens_per_flag; i += 4) {
-    const int token = blockIdx.x * tokens_per_flag + i;
-    if (token >= M) break;
-    float top = kNegInf;
-    for (int b = lane; b < blocks; b += 64) top = fmaxf(top, part[(int64_t)token * part_ld + block0 + b].top);
+// After a piece: references of the next one, and which token blocks have to compute the piece again.  One wave per token.
+__global__ __launch_bounds__(256) void head_check_kernel(const HeadArgs a, int parts, int tokens_per_flag, float* ref_next, int* flag) {
+  const int lane = threadIdx.x & 63, token = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (token >= head_tokens(a)) return;
+  float top = kNegInf;
+  for (int b = lane; b < parts; b += 64) top = fmaxf(top, a.part[(int64_t)token * a.part_ld + a.part0 + b].top);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float r = ref[token];
-    const bool up = top > r + kRaise;
-    if (lane == 0) {
-      ref_next[token] = up ? top : r;
-      if (up) raised = 1;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) flag[blockIdx.x] = raised;
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if (lane != 0) return;
+  const float r = a.ref[token];
+  const bool up = top > r + kRaise;
+  ref_next[token] = up ? top : r;
+  if (up) flag[token / tokens_per_flag] = 1;     // (several may write the same)
 }
 
-// Row results from the parts of all row blocks; for the gradient also 1 - p_t and what turns the sums E into sum p W
-__global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int blocks, const float* ref_last, float* logprob, float* lse, float* entropy,
-                                                          float* rest, float* e_scale) {
+// Row results from all parts; for the gradient also 1 - p_t and what turns the sums E into sum p W, and the slopes of rows without one
+__global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int parts, const int* place, const float* ref_last, float* logprob, float* lse,
+                                                          float* entropy, float* rest, float* e_scale, float* slope, int64_t ld_slope, int64_t H) {
   __shared__ float sm[3][4];
-  const int token = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t target = a.targets[token];
+  const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t target = a.targets[row];
   if (target < 0 || target >= a.V) {
+    const float v = target < 0 ? 0.f : __uint_as_float(0x7fc00000u);
     if (threadIdx.x == 0) {
-      const float v = target < 0 ? 0.f : __uint_as_float(0x7fc00000u);
-      logprob[token] = v;
-      if (lse) lse[token] = v;
-      if (entropy) entropy[token] = v;
-      if (rest) { rest[token] = v; e_scale[token] = 0.f; }
+      logprob[row] = v;
+      if (lse) lse[row] = v;
+      if (entropy) entropy[row] = v;
     }
+    if (slope)
+      for (int64_t h = threadIdx.x; h < H; h += 256) slope[(int64_t)row * ld_slope + h] = v;
     return;
   }
+  const int token = place ? place[row] : row;
   float m = kNegInf, s = 0.f, w = 0.f;
-  for (int b = threadIdx.x; b < blocks; b += 256) {
+  for (int b = threadIdx.x; b < parts; b += 256) {
     const HeadPart p = a.part[(int64_t)token * a.part_ld + b];
     merge_sums(m, s, w, p.ref, p.sum, p.weighted);
   }
@@ -220,26 +235,25 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int 
     l = logf(total);
     logp = kLn2 * (st - m) - l;
   }
-  logprob[token] = logp;
-  if (lse) lse[token] = kLn2 * base + l;
-  if (entropy) entropy[token] = l - kLn2 * w / total;
+  logprob[row] = logp;
+  if (lse) lse[row] = kLn2 * base + l;
+  if (entropy) entropy[row] = l - kLn2 * w / total;
   if (rest) {
-    rest[token] = s / total;
-    e_scale[token] = exp2_fast(ref_last[token] - base) / total;
+    rest[row] = s / total;
+    e_scale[row] = exp2_fast(ref_last[token] - base) / total;
   }
 }
 
-// slope = (1/T) [ (1 - p_t) W_t - sum_{v != t} p_v W_v ]
-__global__ __launch_bounds__(256) void head_slope_kernel(const HeadArgs a, int64_t H, float inv_temperature, const float* rest, const float* e_scale,
-                                                         float* slope, int64_t ld_slope) {
+// slope = (1/T) [ (1 - p_t) W_t - sum_{v != t} p_v W_v ] from the rows kernel's sums
+__global__ __launch_bounds__(256) void head_slope_kernel(const HeadArgs a, const uint16_t* W, int64_t ldw, int64_t H, float inv_temperature, const float* rest,
+                                                         const float* e_scale, float* slope, int64_t ld_slope) {
   const int token = blockIdx.x;
   const int64_t target = a.targets[token];
+  if (target < 0 || target >= a.V) return;
   float* out = slope + (int64_t)token * ld_slope;
   const float r = rest[token], e = e_scale[token];
-  const bool none = target < 0 || target >= a.V;
-  const uint16_t* w = a.a + (none ? 0 : target) * a.lda;
+  const uint16_t* w = W + target * ldw;
   for (int64_t h = threadIdx.x; h < H; h += 256) {
-    if (none) { out[h] = r; continue; }
     float sum = 0.f;
     for (int z = 0; z < a.split; ++z) sum += a.acc[z * a.slab + (int64_t)token * a.ld_acc + h];
     out[h] = inv_temperature * (bf16_bits_to_f32(w[h]) * r - sum * e);
@@ -269,40 +283,65 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(const uint16_t* w, 
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
-constexpr int64_t kMaxHidden = 65535 * 64;
+constexpr int64_t kMaxLd = 1 << 18, kMaxVocab = 1 << 22;  // (exclusive, inclusive) offsets inside the GEMM's operands have 32 bits
 constexpr int64_t kTokenBlock = 8192;                     // tokens that are taken through the whole vocabulary together
 constexpr int64_t kPieceBytes = (int64_t)192 << 20;       // probabilities of a piece: they stay in the last-level cache until they are used
 
 struct HeadPlan {
-  int64_t tokens, blocks, pieces, piece;                  // tokens at a time; row blocks; pieces and their rows (a multiple of 64)
+  HeadGemmPlan gemm;                                      // gemm.tokens == 0: the rows kernel
+  int64_t tokens, parts, part_rows, pieces, piece, flags; // tokens at a time; parts of a row; pieces and their rows (a multiple of 64), flags of a piece
   int split;
-  size_t part, target, ref, flag, rest, p, acc, bytes;    // offsets
+  size_t part, target, index, ref, flag, rest, p, acc, bytes;   // offsets
 };
+
+// Rows of a piece in blocks of `unit`: at most `most`, as few rounds of workgroups as possible over the vocabulary, then as few pieces
+static int64_t piece_blocks(int64_t blocks, int64_t most, int64_t token_blocks) {
+  most = most < 1 ? 1 : most;
+  if (most >= blocks) return blocks;
+  int64_t best = most, best_rounds = INT64_MAX;
+  for (int64_t n = most; n >= 1 && n > most / 2; --n) {
+    const int64_t last = blocks % n, rounds = blocks / n * ceil_div(n * token_blocks, 256) + ceil_div(last * token_blocks, 256);
+    if (rounds < best_rounds) { best = n; best_rounds = rounds; }
+  }
+  return best;
+}
+
 static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
   HeadPlan q = {};
   q.tokens = M < kTokenBlock ? M : kTokenBlock;
-  q.blocks = ceil_div(V, kRowsPerBlock);
+  q.gemm = plan_head_gemm(q.tokens);
+  const bool gemm = q.gemm.tokens > 0;
+  const int64_t row_block = gemm ? q.gemm.rows : kRowsPerBlock, token_block = gemm ? q.gemm.tokens : kTokensPerBlock;
+  q.part_rows = gemm ? q.gemm.part_rows : kRowsPerBlock;
+  q.parts = ceil_div(V, q.part_rows);
   q.pieces = 1;
-  q.piece = q.blocks * kRowsPerBlock;
+  q.piece = ceil_div(V, row_block) * row_block;
   q.split = 1;
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   size_t at = 0;
-  q.part = at; at += up((size_t)(q.tokens * q.blocks) * sizeof(HeadPart));
+  q.part = at; at += up((size_t)(q.tokens * q.parts) * sizeof(HeadPart));
   q.target = at; at += up((size_t)q.tokens * 4);
+  q.index = at; at += gemm ? up((size_t)(2 * q.tokens + 1) * 4) : 0;
   if (gradient) {
-    int64_t rows = kPieceBytes / (2 * q.tokens) / kRowsPerBlock * kRowsPerBlock;
-    rows = rows < kRowsPerBlock ? kRowsPerBlock : rows;
-    q.pieces = ceil_div(q.piece, rows);
-    q.piece = ceil_div(ceil_div(q.piece, q.pieces), kRowsPerBlock) * kRowsPerBlock;
+    const int64_t token_blocks = ceil_div(q.tokens, token_block);
+    q.piece = piece_blocks(ceil_div(V, row_block), kPieceBytes / (2 * token_blocks * token_block * row_block), token_blocks) * row_block;
     q.pieces = ceil_div(V, q.piece);
-    const int64_t groups = ceil_div(H, kRowsPerBlock) * ceil_div(q.tokens, kTokensPerBlock);
-    q.split = (int)(groups >= 512 ? 1 : ceil_div(512, groups));
-    if (q.split > 32) q.split = 32;
+    size_t acc = 0;
+    if (gemm) {
+      const HeadSumsPlan sums = plan_head_sums(q.gemm, q.tokens, H, q.piece, q.pieces);
+      q.split = sums.split;
+      acc = sums.bytes;
+    } else {
+      const int64_t groups = ceil_div(H, kRowsPerBlock) * token_blocks;
+      q.split = (int)(groups >= 512 ? 1 : ceil_div(512, groups) < 32 ? ceil_div(512, groups) : 32);
+      acc = (size_t)(q.split * q.tokens * H) * 4;
+    }
+    q.flags = token_blocks;
     q.ref = at; at += up((size_t)(q.tokens * (q.pieces + 1)) * 4);
-    q.flag = at; at += up((size_t)ceil_div(q.tokens, kTokensPerBlock) * 4);
+    q.flag = at; at += up((size_t)(q.flags * q.pieces) * 4);
     q.rest = at; at += up((size_t)(2 * q.tokens) * 4);
     q.p = at; at += up((size_t)(q.tokens * q.piece) * 2);
-    q.acc = at; at += up((size_t)(q.split * q.tokens * H) * 4);
+    q.acc = at; at += up(acc);
   }
   q.bytes = at;
   return q;
@@ -317,51 +356,72 @@ struct HeadCall {
   uint8_t* ws; size_t ws_bytes; hipStream_t st;
 };
 
+static int launch_rows(HeadMode mode, const HeadArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(a.rows, kRowsPerBlock), (unsigned)ceil_div(a.M, kTokensPerBlock), mode == kSums ? (unsigned)a.split : 1u), block(kKWaves * 64);
+  if (mode == kSums) head_rows_kernel<kSums><<<grid, block, 0, st>>>(a);
+  else if (mode == kProbs) head_rows_kernel<kProbs><<<grid, block, 0, st>>>(a);
+  else head_rows_kernel<kLogits><<<grid, block, 0, st>>>(a);
+  return launch_status();
+}
+
 static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t M) {
+  const bool gemm = q.gemm.tokens > 0;
   HeadArgs a = {};
   a.a = c.W; a.lda = c.ldw; a.rows = c.V; a.b = c.x + m0 * c.ldx; a.ldb = c.ldx; a.k = c.H; a.M = (int)M;
   a.targets = c.targets + m0; a.V = c.V; a.scale = c.inv_temperature * 1.44269504088896341f;
-  a.part = reinterpret_cast<HeadPart*>(c.ws + q.part); a.part_ld = q.blocks; a.target_logit = reinterpret_cast<float*>(c.ws + q.target);
-  const unsigned tb = (unsigned)ceil_div(M, kTokensPerBlock);
+  a.part = reinterpret_cast<HeadPart*>(c.ws + q.part); a.part_ld = q.parts; a.target_logit = reinterpret_cast<float*>(c.ws + q.target);
+  int* place = nullptr;
+  auto launch = [&](HeadMode mode, const HeadArgs& args) {
+    return gemm ? launch_head_gemm(q.gemm, mode, c.entropy != nullptr, args, c.st) : launch_rows(mode, args, c.st);
+  };
+  if (gemm) {
+    int* index = reinterpret_cast<int*>(c.ws + q.index);
+    place = index + q.tokens;
+    head_compact_kernel<<<dim3(1), dim3(kCompactThreads), 0, c.st>>>(a.targets, c.V, (int)M, index, place, place + q.tokens);
+    a.index = index; a.count = place + q.tokens;
+  }
   float* logprob = c.logprob + m0;
   float* lse = c.lse ? c.lse + m0 : nullptr;
   float* entropy = c.entropy ? c.entropy + m0 : nullptr;
   if (!c.slope) {
-    head_rows_kernel<kLogits><<<dim3((unsigned)q.blocks, tb), dim3(kKWaves * 64), 0, c.st>>>(a);
-    head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.blocks, nullptr, logprob, lse, entropy, nullptr, nullptr);
+    if (const int e = launch(kLogits, a)) return e;
+    head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.parts, place, nullptr, logprob, lse, entropy, nullptr, nullptr, nullptr, 0, 0);
     return launch_status();
   }
   float* ref = reinterpret_cast<float*>(c.ws + q.ref);
-  int* flag = reinterpret_cast<int*>(c.ws + q.flag);
+  int* flags = reinterpret_cast<int*>(c.ws + q.flag);
   float* rest = reinterpret_cast<float*>(c.ws + q.rest);
   float* e_scale = rest + q.tokens;
-  const int64_t ldt = ceil_div(c.V, 64) * 64;
-  head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref);
+  float* slope = c.slope + m0 * c.ld_slope;
+  head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref, flags, (int)(q.flags * q.pieces));
   HeadArgs e = a;
-  e.lda = ldt; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
-  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.ld_acc = c.H; e.slab = q.tokens * c.H; e.split = q.split;
+  e.lda = ceil_div(c.V, 64) * 64; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
+  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.ld_acc = c.H; e.split = q.split;
+  e.slab = gemm ? ceil_div(c.H, q.gemm.rows) * ceil_div(q.tokens, q.gemm.tokens) * q.gemm.rows * q.gemm.tokens : q.tokens * c.H;
   for (int64_t i = 0; i < q.pieces; ++i) {
     const int64_t row0 = i * q.piece, rows = c.V - row0 < q.piece ? c.V - row0 : q.piece;
-    a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.block0 = (int)(row0 / kRowsPerBlock);
+    a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.part0 = (int)(row0 / q.part_rows);
     a.p = reinterpret_cast<uint16_t*>(c.ws + q.p); a.ldp = q.piece;
     a.ref = ref + i * q.tokens; a.ref_next = ref + (i + 1) * q.tokens; a.flag = nullptr;
-    const unsigned rb = (unsigned)ceil_div(rows, kRowsPerBlock);
-    head_rows_kernel<kProbs><<<dim3(rb, tb), dim3(kKWaves * 64), 0, c.st>>>(a);
-    head_check_kernel<<<dim3(tb), dim3(256), 0, c.st>>>(a.part, a.part_ld, a.block0, (int)rb, (int)M, kTokensPerBlock, a.ref, ref + (i + 1) * q.tokens, flag);
-    a.flag = flag;
-    head_rows_kernel<kProbs><<<dim3(rb, tb), dim3(kKWaves * 64), 0, c.st>>>(a);
-    e.a = c.Wt + row0; e.k = (int64_t)rb * kRowsPerBlock; e.ref = a.ref; e.ref_next = a.ref_next; e.first = i == 0;
-    head_rows_kernel<kSums><<<dim3((unsigned)ceil_div(c.H, kRowsPerBlock), tb, (unsigned)q.split), dim3(kKWaves * 64), 0, c.st>>>(e);
+    if (const int s = launch(kProbs, a)) return s;
+    head_check_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, (int)ceil_div(rows, q.part_rows), gemm ? q.gemm.tokens : kTokensPerBlock,
+                                                                              ref + (i + 1) * q.tokens, flags + i * q.flags);
+    a.flag = flags + i * q.flags;
+    if (const int s = launch(kProbs, a)) return s;
+    e.a = c.Wt + row0; e.k = ceil_div(rows, 64) * 64; e.ref = a.ref; e.ref_next = a.ref_next; e.first = i == 0;
+    if (const int s = launch(kSums, e)) return s;
   }
-  const float* ref_last = ref + q.pieces * q.tokens;
-  head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.blocks, ref_last, logprob, lse, entropy, rest, e_scale);
-  a.a = c.W; a.acc = e.acc; a.ld_acc = e.ld_acc; a.slab = e.slab; a.split = e.split;
-  head_slope_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, c.H, c.inv_temperature, rest, e_scale, c.slope + m0 * c.ld_slope, c.ld_slope);
+  head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.parts, place, ref + q.pieces * q.tokens, logprob, lse, entropy, rest, e_scale, slope,
+                                                                c.ld_slope, c.H);
+  a.a = c.W;
+  if (gemm) return launch_head_slope(q.gemm, e, a, c.inv_temperature, rest, e_scale, slope, c.ld_slope, c.st);
+  head_slope_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(e, c.W, c.ldw, c.H, c.inv_temperature, rest, e_scale, slope, c.ld_slope);
   return launch_status();
 }
 
 static int run_head(const HeadCall& c, bool gradient) {
-  if (c.M < 0 || c.V < 1 || c.V > 0x7fffffff || c.H < 8 || c.H % 8 != 0 || c.H > kMaxHidden || c.M > 0x7fffffff || c.ldx < c.H || c.ldw < c.H || (gradient && c.ld_slope < c.H))
+  if (c.M < 0 || c.V < 1 || c.V > kMaxVocab || c.H < 8 || c.H % 8 != 0 || c.M > 0x7fffffff || c.ldx < c.H || c.ldx >= kMaxLd || c.ldw < c.H ||
+      c.ldw >= kMaxLd || (gradient && c.ld_slope < c.H))
     return QERL_ERR_SHAPE;
   if (!(c.inv_temperature > 0.f) || !isfinite(c.inv_temperature)) return QERL_ERR_SHAPE;
   if (c.M == 0) return QERL_OK;
@@ -384,7 +444,7 @@ extern "C" size_t lm_head_prepack_t_bytes(int64_t V, int64_t H) {
   return V < 1 || H < 1 ? 0 : (size_t)(ceil_div(V, 64) * 64) * (size_t)H * 2;
 }
 extern "C" int lm_head_prepack_t(const void* W, int64_t V, int64_t H, int64_t ldw, void* Wt, void* stream) {
-  if (V < 0 || H < 0 || V > 0x7fffffff || H % 8 != 0 || H > kMaxHidden || ldw < H) return QERL_ERR_SHAPE;
+  if (V < 0 || H < 0 || V > kMaxVocab || H % 8 != 0 || ldw < H || ldw >= kMaxLd) return QERL_ERR_SHAPE;
   if (V == 0 || H == 0) return QERL_OK;
   if (!W || !Wt) return QERL_ERR_NULL;
   if (!aligned(W, 16) || !aligned(Wt, 16) || ldw % 8) return QERL_ERR_ALIGN;
@@ -395,8 +455,17 @@ extern "C" int lm_head_prepack_t(const void* W, int64_t V, int64_t H, int64_t ld
 }
 
 extern "C" size_t lm_head_logprob_workspace_bytes(int64_t M, int64_t V, int64_t H, int gradient) {
-  if (M < 0 || V < 1 || H < 8 || M > 0x7fffffff || V > 0x7fffffff) return 0;
-  return M == 0 ? 256 : plan_head(M, V, H, gradient != 0).bytes;
+  if (M < 0 || V < 1 || H < 8 || M > 0x7fffffff || V > kMaxVocab || H >= kMaxLd) return 0;
+  size_t most = 256;                             // a smaller call may split its sums further: the largest over all token blocks
+  for (int64_t m : {(int64_t)32, (int64_t)64, (int64_t)128}) {
+    const size_t b = M > 0 ? plan_head(M < m ? M : m, V, H, gradient != 0).bytes : 0;
+    most = b > most ? b : most;
+  }
+  for (int64_t m = 256; m - 256 < M && m <= kTokenBlock; m += 256) {
+    const size_t b = plan_head(M < m ? M : m, V, H, gradient != 0).bytes;
+    most = b > most ? b : most;
+  }
+  return most;
 }
 
 extern "C" int lm_head_logprob(const void* x, int64_t M, int64_t H, int64_t ldx, const void* W, int64_t V, int64_t ldw, const int64_t* targets,
@@ -411,7 +480,7 @@ extern "C" int lm_head_logprob_grad(const void* x, int64_t M, int64_t H, int64_t
                            inv_temperature, logprob, lse, entropy, slope, ld_slope, static_cast<uint8_t*>(ws), ws_bytes, (hipStream_t)stream}, true);
 }
 extern "C" int lm_head_logprob_backward(const float* grad, const float* slope, int64_t ld_slope, int64_t M, int64_t H, void* dx, int64_t lddx, void* stream) {
-  if (M < 0 || M > 0x7fffffff || H < 8 || H % 8 || H > kMaxHidden || ld_slope < H || lddx < H) return QERL_ERR_SHAPE;
+  if (M < 0 || M > 0x7fffffff || H < 8 || H % 8 || H > 0x7fffffff || ld_slope < H || lddx < H) return QERL_ERR_SHAPE;
   if (M == 0) return QERL_OK;
   if (!grad || !slope || !dx) return QERL_ERR_NULL;
   if (!aligned(grad, 4) || !aligned(slope, 16) || !aligned(dx, 16) || ld_slope % 4 || lddx % 8) return QERL_ERR_ALIGN;

@@ -4,27 +4,48 @@
 
 namespace qerl {
 
-// One row block of the vocabulary seen by one token: with s = logit * log2(e), others = every row of the block but the token's own,
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kRaise = 60.f;                  // a logit this far (in powers of two) above the reference raises it
+
+// Some rows of the vocabulary seen by one token: with s = logit * log2(e), others = all of these rows but the token's own,
 //   ref: what the sums are relative to, sum = sum_others 2^(s - ref), weighted = sum_others 2^(s - ref) (s - ref), top = max_others s
 struct HeadPart { float ref, sum, weighted, top; };
 
+enum HeadMode { kLogits, kProbs, kSums };
+
 struct HeadArgs {
-  const uint16_t* a; int64_t lda, rows;         // row operand [rows, k]: W (rows = vocabulary), or its transpose (rows = hidden)
+  const uint16_t* a; int64_t lda, rows;         // row operand [rows, k]: W (rows = vocabulary) or its transpose (rows = hidden)
   const uint16_t* b; int64_t ldb;               // token operand [tokens, k]: x, or the piece's probabilities
-  int64_t k; int M;                             // contraction length; tokens
+  int64_t k; int M;                             // contraction length; tokens at most
+  const int* index; const int* count;           // rows of x and targets that the tokens stand for, and how many there are; null: all M as they come
   const int64_t* targets; int64_t V;
   float scale;                                  // log2(e) / temperature
-  HeadPart* part; int64_t part_ld;              // [tokens][part_ld] row blocks
+  HeadPart* part; int64_t part_ld;              // [tokens][part_ld]
   float* target_logit;                          // [tokens] s of the token's own row
-  int64_t row0;                                 // vocabulary row of a's first row (a piece of the vocabulary)
-  int block0;                                   // row block of a's first row in `part`
+  int64_t row0; int part0;                      // a's first row in the vocabulary, its first part
   // pieces (gradient)
   uint16_t* p; int64_t ldp;                     // probabilities 2^(s - ref) of the piece, 0 at the token's own row and beyond the vocabulary
-  const float* ref; const float* ref_next;      // [tokens] the references of this piece and of the next (raised where a logit passed it by far)
-  const int* flag;                              // [token blocks] piece has to be computed again with ref_next; null: first computation
-  float* acc; int64_t ld_acc; int64_t slab;     // sums E [split][tokens][ld_acc]
+  const float* ref; const float* ref_next;      // [tokens] the references of this piece and of the next (raised where a logit passed them by far)
+  const int* flag;                              // [token blocks] which compute the piece again, with ref_next; null: first computation
+  float* acc; int64_t ld_acc; int64_t slab;     // sums E: [split][tokens][ld_acc] (rows kernel), [split][tiles][tile] (GEMM)
   int first;                                    // the sums start here
   int split;
 };
+__device__ __forceinline__ int head_tokens(const HeadArgs& a) { return a.count ? *a.count : a.M; }
+__device__ __forceinline__ int head_row(const HeadArgs& a, int token) { return a.index ? a.index[token] : token; }
+
+// the GEMM kernels (lm_head_gemm.hip)
+struct HeadGemmPlan {
+  int tokens;                                   // tokens of a tile: 128 or 256; 0: the GEMM does not take the call
+  int rows, part_rows;                          // vocabulary rows of a tile, of a part
+};
+HeadGemmPlan plan_head_gemm(int64_t M);
+int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st);
+// the sums: how K is split, what the partial sums take, and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
+struct HeadSumsPlan { int split; int64_t row_blocks, token_blocks; size_t bytes; };
+HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces);
+int launch_head_slope(const HeadGemmPlan& p, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale,
+                      float* slope, int64_t ld_slope, hipStream_t st);
 
 }  // namespace qerl

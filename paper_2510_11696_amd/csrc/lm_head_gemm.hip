@@ -1,0 +1,451 @@
+// The head's matrix products for more than a few tokens: logits of a piece of the vocabulary with their row statistics (and their
+// probabilities, kept as bf16 for the piece only), and the sums E = P W over a piece.
+//
+// A workgroup of eight waves owns 256 rows x 256 tokens, a wave 128 x 64 of them.  Stages of 64 inputs: both operands go from memory to LDS
+// directly, row slabs two stages ahead (they come from HBM), token slabs one (they sit in the caches); the workgroup meets once a stage,
+// three quarters into it, when the next slabs are needed, so that the first fragments of the next stage are read between the last
+// quarter's matrix instructions.
+//
+// Operand layout in LDS: rows of 64 inputs as eight 16-byte chunks, chunk c of row r at r * 8 + (c ^ ((r >> 1) & 7)).
+#include "lm_head.hpp"
+#include "lds_dma.hpp"
+#include "tile_out.hpp"
+
+namespace qerl {
+
+// RT row tiles and TT token tiles of 32 per wave, WR x WT waves, SA and SB slabs of the operands in LDS
+template <int RT_, int TT_, int WR_, int WT_, int SA_, int SB_>
+struct HeadCfg {
+  static constexpr int RT = RT_, TT = TT_, WR = WR_, WT = WT_, SA = SA_, SB = SB_;
+  static constexpr int kWaves = WR * WT, kThreads = 64 * kWaves, kRows = 32 * RT * WR, kTokens = 32 * TT * WT;
+  static constexpr int kSlabA = kRows * 8, kSlabB = kTokens * 8;                // 16-byte chunks
+  static constexpr int IA = kSlabA / kThreads, IB = kSlabB / kThreads;          // requests per wave and stage
+  static_assert(IA * kThreads == kSlabA && IB * kThreads == kSlabB, "whole requests");
+  static constexpr int kLdsSlabs = (SA * kSlabA + SB * kSlabB) * 16, kLdsOut = kWaves * tile_out_bytes(RT);
+  static constexpr int kLds = kLdsSlabs > kLdsOut ? kLdsSlabs : kLdsOut;
+  static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+  // requests that may be outstanding when stage s + 1 is needed: those behind its own, batches being (token slab, row slab)
+  static constexpr int kAfterB = IA + (SB - 2) * (IA + IB), kAfterA = (SA - 2) * (IA + IB);
+  static constexpr int kAhead = kAfterA < kAfterB ? kAfterA : kAfterB;
+  static constexpr int kDeep = SA > SB ? SA : SB;
+};
+
+// Stages [s0, s1) of a tile's product, added to acc.  rows_a / rows_b: byte offsets of the lane's rows for each request.
+template <class C>
+struct HeadLoop {
+  u32x4* lds;
+  uint32_t lds0;
+  int lane, wave, wr, wt, n32, kg;
+  const uint8_t* base_a; const uint8_t* base_b;
+  uint32_t off_a[C::IA], off_b[C::IB];
+  int64_t k;
+
+  __device__ __forceinline__ void init(u32x4* memory, int tid) {
+    lds = memory; lds0 = lds_address(memory);
+    lane = tid & 63; wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    wr = wave % C::WR; wt = wave / C::WR;
+    n32 = lane & 31; kg = lane >> 5;
+  }
+  __device__ __forceinline__ int slab_row(int i) const { return wave * 8 + (lane >> 3) + 8 * C::kWaves * i; }
+  __device__ __forceinline__ uint32_t slab_col() const { return (uint32_t)(((lane & 7) ^ ((slab_row(0) >> 1) & 7)) * 16); }
+  template <int N>
+  __device__ __forceinline__ void request(const uint8_t* base, const uint32_t (&off)[N], int slab_chunks, int stage) {
+    const uint32_t dst = lds0 + (uint32_t)((slab_chunks + wave * 64) * 16);
+    const uint8_t* p = base + (int64_t)stage * 128;
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds_request(dst + (uint32_t)(i * C::kThreads * 16), p, off[i]);
+  }
+  // the last stage of a k that is no multiple of 64: through registers, zeros behind k (which is a multiple of 8)
+  template <int N>
+  __device__ __forceinline__ void copy_tail(const uint8_t* base, const uint32_t (&off)[N], int slab_chunks, int stage) {
+    const bool inside = (int64_t)stage * 128 + slab_col() < k * 2;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(base + off[i] + (inside ? (int64_t)stage * 128 : -(int64_t)slab_col()));
+      lds[slab_chunks + i * C::kThreads + wave * 64 + lane] = inside ? v : u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ int chunk_a(int slot, int j, int t) const {
+    const int r = n32;
+    return slot + (wr * C::RT * 32 + r) * 8 + ((2 * j + kg) ^ ((r >> 1) & 7)) + t * 256;
+  }
+  __device__ __forceinline__ int chunk_b(int slot, int j, int t) const {
+    const int r = n32;
+    return slot + C::SA * C::kSlabA + (wt * C::TT * 32 + r) * 8 + ((2 * j + kg) ^ ((r >> 1) & 7)) + t * 256;
+  }
+  __device__ __forceinline__ bf16x8 frag(int chunk) const { return __builtin_bit_cast(bf16x8, lds[chunk]); }
+
+  __device__ __forceinline__ void run(f32x16 (&acc)[C::RT][C::TT], int s0, int s1) {
+    const int full = (int)(k >> 6);              // stages from here on take the tail's way
+    int next_a = s0, next_b = s0;                // next stages to fetch
+    int put_a = 0, put_b = 0;                    // their slots
+    auto fetch_a = [&] {
+      if (next_a < s1) {
+        if (next_a < full) request(base_a, off_a, put_a, next_a); else copy_tail(base_a, off_a, put_a, next_a);
+        ++next_a;
+        put_a = put_a + C::kSlabA == C::SA * C::kSlabA ? 0 : put_a + C::kSlabA;
+      }
+    };
+    auto fetch_b = [&] {
+      if (next_b < s1) {
+        const int at = C::SA * C::kSlabA + put_b;
+        if (next_b < full) request(base_b, off_b, at, next_b); else copy_tail(base_b, off_b, at, next_b);
+        ++next_b;
+        put_b = put_b + C::kSlabB == C::SB * C::kSlabB ? 0 : put_b + C::kSlabB;
+      }
+    };
+    // before the first stage: SB - 1 token slabs and SA - 1 row slabs, the last batch (token, row)
+#pragma unroll
+    for (int i = 0; i < C::kDeep - 1; ++i) {
+      if (i >= C::kDeep - C::SB) fetch_b();
+      if (i >= C::kDeep - C::SA) fetch_a();
+    }
+    auto meet = [&](int s) {                     // everybody has read stage s - 1, and stage s is in LDS
+      if (s + C::kDeep - 2 < (s1 < full ? s1 : full)) lds_wait_barrier<C::kAhead>();
+      else lds_wait_barrier<0>();
+    };
+    meet(s0);
+    fetch_b();
+    fetch_a();
+    int slot_a = 0, slot_b = 0;
+    bf16x8 fa[C::RT], fb[C::TT];
+#pragma unroll
+    for (int t = 0; t < C::TT; ++t) fb[t] = frag(chunk_b(slot_b, 0, t));
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) fa[t] = frag(chunk_a(slot_a, 0, t));
+    for (int s = s0; s < s1; ++s) {
+      const int after_a = slot_a + C::kSlabA == C::SA * C::kSlabA ? 0 : slot_a + C::kSlabA;
+      const int after_b = slot_b + C::kSlabB == C::SB * C::kSlabB ? 0 : slot_b + C::kSlabB;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j == 3 && s + 1 < s1) {
+          __builtin_amdgcn_sched_barrier(0);
+          meet(s + 1);
+          fetch_b();
+          fetch_a();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        const int ca = j < 3 ? slot_a : after_a, cb = j < 3 ? slot_b : after_b, jn = (j + 1) & 3;
+        bf16x8 na[C::RT], nb[C::TT];
+#pragma unroll
+        for (int t = 0; t < C::TT; ++t) nb[t] = frag(chunk_b(cb, jn, t));     // behind the last stage: whatever the slot holds, not used
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t) na[t] = frag(chunk_a(ca, jn, t));
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+          for (int tt = 0; tt < C::TT; ++tt) acc[t][tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[t], fb[tt], acc[t][tt], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < C::RT; ++t) fa[t] = na[t];
+#pragma unroll
+        for (int t = 0; t < C::TT; ++t) fb[t] = nb[t];
+#pragma unroll
+        for (int i = 0; i < C::RT + C::TT; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      slot_a = after_a;
+      slot_b = after_b;
+    }
+  }
+};
+
+// Row statistics of a wave's tile, from the products in acc; with PROBS acc becomes 2^(s - ref).
+// lane l holds of token 32 tt + l % 32 the rows 32 t + 8 q + 4 (l / 32) + 0..3 as elements 4 q .. 4 q + 3
+template <class C, bool PROBS, bool ENTROPY>
+__device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], const HeadArgs& a, int M, int64_t r0, int m0, int part, int lane) {
+  const int n32 = lane & 31, kg = lane >> 5;
+  const float scale = a.scale;
+#pragma unroll
+  for (int tt = 0; tt < C::TT; ++tt) {
+    const int token = m0 + tt * 32 + n32;
+    const bool live = token < M;
+    const int at = live ? token : M - 1;
+    const int64_t far = a.targets[head_row(a, at)] - a.row0 - r0;              // the token's own row, in the tile?
+    const bool mine = far >= 0 && far < 32 * C::RT && (((int)far >> 2) & 1) == kg;
+    if (__any(mine)) {
+      const int own = mine ? (int)far - 4 * kg : -1;
+      float logit = 0.f;
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool hit = own == t * 32 + 8 * (i >> 2) + (i & 3);
+          logit = hit ? acc[t][tt][i] : logit;
+          acc[t][tt][i] = hit ? kNegInf : acc[t][tt][i];
+        }
+      if (mine && live) a.target_logit[token] = logit * scale;
+    }
+    if (r0 + 32 * C::RT > a.rows) {
+      const int end = (int)(a.rows - r0) - 4 * kg;
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[t][tt][i] = t * 32 + 8 * (i >> 2) + (i & 3) < end ? acc[t][tt][i] : kNegInf;
+    }
+    float top = kNegInf;
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[t][tt][i]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;
+    const float ref = PROBS ? (a.flag ? a.ref_next : a.ref)[at] : top;
+    const float base = PROBS ? ref : top == kNegInf ? 0.f : top;
+    float sum[2] = {0.f, 0.f}, weighted[2] = {0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float d = fmaf(acc[t][tt][i], scale, -base), e = __builtin_amdgcn_exp2f(d);
+        sum[i & 1] += e;
+        if (ENTROPY) weighted[i & 1] = fmaf(e, fmaxf(d, -1e30f), weighted[i & 1]);     // (0 at rows that do not count, where d is -inf)
+        if (PROBS) acc[t][tt][i] = e;
+      }
+    float s = sum[0] + sum[1], w = weighted[0] + weighted[1];
+    s += __shfl_xor(s, 32, 64);
+    if (ENTROPY) w += __shfl_xor(w, 32, 64);
+    if (live && kg == 0) a.part[(int64_t)token * a.part_ld + part] = HeadPart{ref, s, w, top};
+  }
+}
+
+template <class C, bool PROBS, bool ENTROPY>
+__global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_gemm_kernel(const HeadArgs a, int row_blocks, int blocks_per_xcd) {
+  extern __shared__ __attribute__((aligned(256))) u32x4 head_lds[];
+  HeadLoop<C> loop;
+  loop.init(head_lds, threadIdx.x);
+  loop.k = a.k;
+  const int M = head_tokens(a), token_blocks = (M + C::kTokens - 1) / C::kTokens;
+  const int stages = (int)((a.k + 63) >> 6), total = 8 * blocks_per_xcd * token_blocks;
+  for (int tile = blockIdx.x; tile < total; tile += gridDim.x) {
+    // workgroup ids go round-robin to the eight XCDs, each of which takes a contiguous eighth of the row blocks; four of them and all
+    // token blocks, rows first, make a group, so that what is in flight on an XCD shares its slabs
+    const int xcd = tile & 7, local = tile >> 3, group = local / (4 * token_blocks), in = local - group * 4 * token_blocks;
+    const int width = blocks_per_xcd - 4 * group < 4 ? blocks_per_xcd - 4 * group : 4;
+    const int mb = in / width, rb = xcd * blocks_per_xcd + 4 * group + in - mb * width;
+    if (rb >= row_blocks) continue;
+    if (PROBS && a.flag && !a.flag[mb]) continue;
+    const int64_t r0 = (int64_t)rb * C::kRows;
+    const int m0 = mb * C::kTokens;
+    loop.base_a = uniform_pointer(a.a + r0 * a.lda);
+    loop.base_b = uniform_pointer(a.b);
+#pragma unroll
+    for (int i = 0; i < C::IA; ++i) {
+      const int64_t r = r0 + loop.slab_row(i) < a.rows ? loop.slab_row(i) : a.rows - 1 - r0;
+      loop.off_a[i] = (uint32_t)(r * a.lda * 2) + loop.slab_col();
+    }
+#pragma unroll
+    for (int i = 0; i < C::IB; ++i) {
+      const int token = m0 + loop.slab_row(i);
+      loop.off_b[i] = (uint32_t)((int64_t)head_row(a, token < M ? token : M - 1) * a.ldb * 2) + loop.slab_col();
+    }
+    f32x16 acc[C::RT][C::TT];
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+      for (int tt = 0; tt < C::TT; ++tt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
+    loop.run(acc, 0, stages);
+    const int64_t wr0 = r0 + loop.wr * C::RT * 32;
+    const int wm0 = m0 + loop.wt * C::TT * 32;
+    if (wr0 < a.rows) head_statistics<C, PROBS, ENTROPY>(acc, a, M, wr0, wm0, a.part0 + rb * C::WR + loop.wr, loop.lane);
+    if constexpr (PROBS) {
+      lds_wait_barrier<0>();                       // nobody reads slabs any more
+      if (wr0 < a.rows)
+        store_tiles<C::TT, C::RT>(acc, 1.f, nullptr, a.p, a.ldp, M, (a.rows + 63) & ~(int64_t)63, wm0, wr0,
+                                  reinterpret_cast<uint8_t*>(head_lds) + loop.wave * tile_out_bytes(C::RT), loop.lane);
+    }
+    if (tile + (int)gridDim.x < total) lds_wait_barrier<0>();                  // before the next tile's requests
+  }
+}
+
+// ---- sums: [tokens, piece] x [piece, H] ----------------------------------------------------------------------------------
+// Unit u of `split` x tiles: which K-part, row block and token block.  The eight XCDs share the K-parts out (several of them to a part
+// where there are fewer than eight), and inside a part the tiles, so that an XCD's caches see few slabs.
+struct HeadUnit { int part, rb, mb; bool any; };
+__device__ __forceinline__ HeadUnit head_unit(int xcd, int local, int split, int row_blocks, int token_blocks) {
+  const int tiles = row_blocks * token_blocks;
+  if (split >= 8) {
+    const int turn = local / tiles, in = local - turn * tiles, part = turn * 8 + xcd;
+    return HeadUnit{part, in % row_blocks, in / row_blocks, part < split};
+  }
+  const int xs = 8 / split, part = xcd / xs, x = xcd % xs;             // xs XCDs take the tiles of a part: 1, 2 x 1, 2 x 2 or 4 x 2 of rows x tokens
+  const int xr = xs >= 8 ? 4 : xs >= 2 ? 2 : 1, xt = xs / xr;
+  const int nr = (row_blocks + xr - 1) / xr, nt = (token_blocks + xt - 1) / xt;
+  const int rb = (x % xr) * nr + local % nr, mb = (x / xr) * nt + local / nr;
+  return HeadUnit{part, rb, mb, local < nr * nt && local % nr + (x % xr) * nr < row_blocks && mb < token_blocks};
+}
+__host__ __device__ inline int head_units_per_xcd(int split, int row_blocks, int token_blocks) {
+  if (split >= 8) return (split + 7) / 8 * row_blocks * token_blocks;
+  const int xs = 8 / split, xr = xs >= 8 ? 4 : xs >= 2 ? 2 : 1, xt = xs / xr;
+  return ((row_blocks + xr - 1) / xr) * ((token_blocks + xt - 1) / xt);
+}
+
+template <class C>
+__global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_sums_kernel(const HeadArgs a, int row_blocks) {
+  extern __shared__ __attribute__((aligned(256))) u32x4 head_lds[];
+  HeadLoop<C> loop;
+  loop.init(head_lds, threadIdx.x);
+  loop.k = a.k;
+  const int M = head_tokens(a), token_blocks = (M + C::kTokens - 1) / C::kTokens;
+  if (M == 0) return;
+  const int stages = (int)(a.k >> 6);
+  const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+  const HeadUnit u = head_unit(xcd, local, a.split, row_blocks, token_blocks);
+  if (!u.any) return;
+  const int s0 = (int)((int64_t)stages * u.part / a.split), s1 = (int)((int64_t)stages * (u.part + 1) / a.split);
+  const int64_t r0 = (int64_t)u.rb * C::kRows;
+  const int m0 = u.mb * C::kTokens;
+  loop.base_a = uniform_pointer(a.a + r0 * a.lda);
+  loop.base_b = uniform_pointer(a.b + (int64_t)m0 * a.ldb);
+#pragma unroll
+  for (int i = 0; i < C::IA; ++i) {
+    const int64_t r = r0 + loop.slab_row(i) < a.rows ? loop.slab_row(i) : a.rows - 1 - r0;
+    loop.off_a[i] = (uint32_t)(r * a.lda * 2) + loop.slab_col();
+  }
+#pragma unroll
+  for (int i = 0; i < C::IB; ++i) {
+    const int token = m0 + loop.slab_row(i) < M ? loop.slab_row(i) : M - 1 - m0;
+    loop.off_b[i] = (uint32_t)((int64_t)token * a.ldb * 2) + loop.slab_col();
+  }
+  f32x16 acc[C::RT][C::TT];
+#pragma unroll
+  for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+    for (int tt = 0; tt < C::TT; ++tt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
+  if (s1 > s0) loop.run(acc, s0, s1);
+  // partial sums stay in the registers' order: lane after lane, four rows of a token each
+  f32x4* out = reinterpret_cast<f32x4*>(a.acc + u.part * a.slab) + ((int64_t)(u.mb * row_blocks + u.rb) * C::kWaves + loop.wave) * (C::RT * C::TT * 4 * 64) + loop.lane;
+#pragma unroll
+  for (int tt = 0; tt < C::TT; ++tt) {
+    int token = m0 + (loop.wt * C::TT + tt) * 32 + loop.n32;
+    token = token < M ? token : M - 1;
+    const float r = a.ref[token], rn = a.ref_next[token], alpha = r == rn ? 1.f : __builtin_amdgcn_exp2f(r - rn);
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4* o = out + (int64_t)((tt * C::RT + t) * 4 + q) * 64;
+        f32x4 v = {acc[t][tt][4 * q], acc[t][tt][4 * q + 1], acc[t][tt][4 * q + 2], acc[t][tt][4 * q + 3]};
+        if (!a.first) {
+          const f32x4 old = *o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(alpha, old[e], v[e]);
+        }
+        *o = v;
+      }
+  }
+}
+
+// slope = (1/T) [ (1 - p_t) W_t - sums e_scale ]; one workgroup per wave's part of a tile
+template <class C>
+__global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadArgs a, const uint16_t* W, int64_t ldw, int row_blocks, float inv_temperature,
+                                                                     const float* rest, const float* e_scale, float* slope, int64_t ld_slope) {
+  const int M = head_tokens(a);
+  const int wave = blockIdx.x % C::kWaves, tile = blockIdx.x / C::kWaves, rb = tile % row_blocks, mb = tile / row_blocks;
+  const int wr = wave % C::WR, wt = wave / C::WR, lane = threadIdx.x & 63, tt = threadIdx.x >> 6;
+  const int token = mb * C::kTokens + (wt * C::TT + tt) * 32 + (lane & 31);
+  if (token >= M) return;
+  const int row = head_row(a, token);
+  const int64_t h0 = (int64_t)rb * C::kRows + wr * C::RT * 32 + 4 * (lane >> 5);
+  const float r = rest[row] * inv_temperature, es = e_scale[row] * inv_temperature;
+  const uint16_t* w = W + a.targets[row] * ldw;
+  float* out = slope + (int64_t)row * ld_slope;
+  const f32x4* in = reinterpret_cast<const f32x4*>(a.acc) + ((int64_t)tile * C::kWaves + wave) * (C::RT * C::TT * 4 * 64) + lane;
+#pragma unroll
+  for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t h = h0 + t * 32 + 8 * q;
+      if (h >= a.rows) continue;                   // H is a multiple of 8: four rows are inside or beyond
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      for (int z = 0; z < a.split; ++z) s += in[z * (a.slab / 4) + (int64_t)((tt * C::RT + t) * 4 + q) * 64];
+      const u32x2 wv = *reinterpret_cast<const u32x2*>(w + h);
+      f32x4 o;
+      o[0] = bf16_bits_to_f32(wv[0] & 0xffffu) * r - s[0] * es;
+      o[1] = __uint_as_float(wv[0] & 0xffff0000u) * r - s[1] * es;
+      o[2] = bf16_bits_to_f32(wv[1] & 0xffffu) * r - s[2] * es;
+      o[3] = __uint_as_float(wv[1] & 0xffff0000u) * r - s[3] * es;
+      *reinterpret_cast<f32x4*>(out + h) = o;
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+using Head256 = HeadCfg<4, 2, 2, 4, 3, 2>;       // 256 rows x 256 tokens
+using Head128 = HeadCfg<2, 2, 4, 2, 3, 2>;       // 256 rows x 128 tokens
+
+HeadGemmPlan plan_head_gemm(int64_t M) {
+  if (M <= 64) return HeadGemmPlan{0, 0, 0};
+  // a token block of 128 leaves less unused where 256 would be half empty
+  if (M <= 128) return HeadGemmPlan{Head128::kTokens, Head128::kRows, 32 * Head128::RT};
+  return HeadGemmPlan{Head256::kTokens, Head256::kRows, 32 * Head256::RT};
+}
+
+template <class K>
+static int allow_lds(K kernel, int bytes) {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) { set_last_hip_error((int)e); return QERL_ERR_LAUNCH; }
+  return QERL_OK;
+}
+
+template <class C, bool PROBS, bool ENTROPY>
+static int launch_products(const HeadArgs& a, hipStream_t st) {
+  if (const int e = allow_lds(head_gemm_kernel<C, PROBS, ENTROPY>, C::kLds)) return e;
+  const int row_blocks = (int)ceil_div(a.rows, C::kRows), per_xcd = (int)ceil_div(row_blocks, 8);
+  int64_t grid = 8 * (int64_t)per_xcd * ceil_div(a.M, C::kTokens);
+  if (a.flag && grid > 256) grid = 256;          // hardly ever anything to do: a few workgroups look at all tiles
+  head_gemm_kernel<C, PROBS, ENTROPY><<<dim3((unsigned)grid), dim3(C::kThreads), C::kLds, st>>>(a, row_blocks, per_xcd);
+  return launch_status();
+}
+template <class C>
+static int launch_sums(const HeadArgs& a, hipStream_t st) {
+  if (const int e = allow_lds(head_sums_kernel<C>, C::kLds)) return e;
+  const int row_blocks = (int)ceil_div(a.rows, C::kRows), units = head_units_per_xcd(a.split, row_blocks, (int)ceil_div(a.M, C::kTokens));
+  head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLds, st>>>(a, row_blocks);
+  return launch_status();
+}
+template <class C>
+static int launch_mode(HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st) {
+  if (mode == kSums) return launch_sums<C>(a, st);
+  if (mode == kProbs) return entropy ? launch_products<C, true, true>(a, st) : launch_products<C, true, false>(a, st);
+  return entropy ? launch_products<C, false, true>(a, st) : launch_products<C, false, false>(a, st);
+}
+int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st) {
+  return p.tokens == Head256::kTokens ? launch_mode<Head256>(mode, entropy, a, st) : launch_mode<Head128>(mode, entropy, a, st);
+}
+
+// The split that costs least: rounds of units over the chip's 256 compute units, 0.9 us a stage, and the partial sums, which every piece
+// reads and writes at 5 TB/s.
+HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces) {
+  HeadSumsPlan q = {1, ceil_div(H, p.rows), ceil_div(M, p.tokens), 0};
+  const double tile_bytes = 4.0 * p.rows * p.tokens, stage_us = 0.9 * p.tokens / 256;
+  double best = 1e30;
+  for (int split = 1; split <= 64 && split <= piece / 64; split *= 2) {
+    const int units = head_units_per_xcd(split, (int)q.row_blocks, (int)q.token_blocks);
+    const double us = (double)ceil_div(units, 32) * (double)ceil_div(piece / 64, split) * stage_us +
+                      (double)(q.row_blocks * q.token_blocks * split) * tile_bytes * (pieces > 1 ? 2 : 1) / 5e6;
+    if (us < best * 0.98) { best = us; q.split = split; }
+  }
+  q.bytes = (size_t)(q.split * q.row_blocks * q.token_blocks) * 4 * (size_t)(p.rows * p.tokens);
+  return q;
+}
+
+template <class C>
+static int launch_slope(const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale, float* slope, int64_t ld_slope,
+                        hipStream_t st) {
+  const int row_blocks = (int)ceil_div(sums.rows, C::kRows);
+  head_tile_slope_kernel<C><<<dim3((unsigned)(row_blocks * ceil_div(sums.M, C::kTokens) * C::kWaves)), dim3(64 * C::TT), 0, st>>>(
+      sums, head.a, head.lda, row_blocks, inv_temperature, rest, e_scale, slope, ld_slope);
+  return launch_status();
+}
+int launch_head_slope(const HeadGemmPlan& p, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale,
+                      float* slope, int64_t ld_slope, hipStream_t st) {
+  return p.tokens == Head256::kTokens ? launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+                                      : launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
+}
+
+}  // namespace qerl
