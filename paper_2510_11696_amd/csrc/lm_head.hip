@@ -289,6 +289,7 @@ constexpr int64_t kPieceBytes = (int64_t)192 << 20;       // probabilities of a 
 
 struct HeadPlan {
   HeadGemmPlan gemm;                                      // gemm.tokens == 0: the rows kernel
+  HeadSumsPlan sums;
   int64_t tokens, parts, part_rows, pieces, piece, flags; // tokens at a time; parts of a row; pieces and their rows (a multiple of 64), flags of a piece
   int split;
   size_t part, target, index, ref, flag, rest, p, acc, bytes;   // offsets
@@ -328,9 +329,9 @@ static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
     q.pieces = ceil_div(V, q.piece);
     size_t acc = 0;
     if (gemm) {
-      const HeadSumsPlan sums = plan_head_sums(q.gemm, q.tokens, H, q.piece, q.pieces);
-      q.split = sums.split;
-      acc = sums.bytes;
+      q.sums = plan_head_sums(q.gemm, q.tokens, H, q.piece, q.pieces);
+      q.split = q.sums.split;
+      acc = q.sums.bytes;
     } else {
       const int64_t groups = ceil_div(H, kRowsPerBlock) * token_blocks;
       q.split = (int)(groups >= 512 ? 1 : ceil_div(512, groups) < 32 ? ceil_div(512, groups) : 32);
@@ -397,7 +398,7 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
   HeadArgs e = a;
   e.lda = ceil_div(c.V, 64) * 64; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
   e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.ld_acc = c.H; e.split = q.split;
-  e.slab = gemm ? ceil_div(c.H, q.gemm.rows) * ceil_div(q.tokens, q.gemm.tokens) * q.gemm.rows * q.gemm.tokens : q.tokens * c.H;
+  e.slab = gemm ? ceil_div(c.H, q.sums.rows) * ceil_div(q.tokens, q.gemm.tokens) * q.sums.rows * q.gemm.tokens : q.tokens * c.H;
   for (int64_t i = 0; i < q.pieces; ++i) {
     const int64_t row0 = i * q.piece, rows = c.V - row0 < q.piece ? c.V - row0 : q.piece;
     a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.part0 = (int)(row0 / q.part_rows);
@@ -409,12 +410,12 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
     a.flag = flags + i * q.flags;
     if (const int s = launch(kProbs, a)) return s;
     e.a = c.Wt + row0; e.k = ceil_div(rows, 64) * 64; e.ref = a.ref; e.ref_next = a.ref_next; e.first = i == 0;
-    if (const int s = launch(kSums, e)) return s;
+    if (const int s = gemm ? launch_head_sums(q.gemm, q.sums, e, c.st) : launch_rows(kSums, e, c.st)) return s;
   }
   head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.parts, place, ref + q.pieces * q.tokens, logprob, lse, entropy, rest, e_scale, slope,
                                                                 c.ld_slope, c.H);
   a.a = c.W;
-  if (gemm) return launch_head_slope(q.gemm, e, a, c.inv_temperature, rest, e_scale, slope, c.ld_slope, c.st);
+  if (gemm) return launch_head_slope(q.gemm, q.sums, e, a, c.inv_temperature, rest, e_scale, slope, c.ld_slope, c.st);
   head_slope_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(e, c.W, c.ldw, c.H, c.inv_temperature, rest, e_scale, slope, c.ld_slope);
   return launch_status();
 }

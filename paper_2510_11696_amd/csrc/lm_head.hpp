@@ -41,11 +41,12 @@ struct HeadGemmPlan {
   int rows, part_rows;                          // vocabulary rows of a tile, of a part
 };
 HeadGemmPlan plan_head_gemm(int64_t M);
-int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st);
-// the sums: how K is split, what the partial sums take, and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
-struct HeadSumsPlan { int split; int64_t row_blocks, token_blocks; size_t bytes; };
+int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st);      // kLogits, kProbs
+// the sums: rows of a tile, how K is split, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
+struct HeadSumsPlan { int rows, split; size_t bytes; };
 HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces);
-int launch_head_slope(const HeadGemmPlan& p, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale,
-                      float* slope, int64_t ld_slope, hipStream_t st);
+int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st);
+int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest,
+                      const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st);
 
 }  // namespace qerl

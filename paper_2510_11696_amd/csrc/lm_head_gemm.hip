@@ -22,8 +22,8 @@ struct HeadCfg {
   static constexpr int IA = kSlabA / kThreads, IB = kSlabB / kThreads;          // requests per wave and stage
   static_assert(IA * kThreads == kSlabA && IB * kThreads == kSlabB, "whole requests");
   static constexpr int kLdsSlabs = (SA * kSlabA + SB * kSlabB) * 16, kLdsOut = kWaves * tile_out_bytes(RT);
-  static constexpr int kLds = kLdsSlabs > kLdsOut ? kLdsSlabs : kLdsOut;
-  static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+  static constexpr int kLdsProducts = kLdsSlabs > kLdsOut ? kLdsSlabs : kLdsOut;
+  static_assert(kLdsSlabs <= 160 * 1024, "LDS of a compute unit");
   // requests that may be outstanding when stage s + 1 is needed: those behind its own, batches being (token slab, row slab)
   static constexpr int kAfterB = IA + (SB - 2) * (IA + IB), kAfterA = (SA - 2) * (IA + IB);
   static constexpr int kAhead = kAfterA < kAfterB ? kAfterA : kAfterB;
@@ -39,6 +39,7 @@ struct HeadLoop {
   const uint8_t* base_a; const uint8_t* base_b;
   uint32_t off_a[C::IA], off_b[C::IB];
   int64_t k;
+  bool active;                                   // the wave has tokens (uniform)
 
   __device__ __forceinline__ void init(u32x4* memory, int tid) {
     lds = memory; lds0 = lds_address(memory);
@@ -107,6 +108,14 @@ struct HeadLoop {
     meet(s0);
     fetch_b();
     fetch_a();
+    if (!active) {                               // no tokens for this wave: it fetches and meets only
+      for (int s = s0 + 1; s < s1; ++s) {
+        meet(s);
+        fetch_b();
+        fetch_a();
+      }
+      return;
+    }
     int slot_a = 0, slot_b = 0;
     bf16x8 fa[C::RT], fb[C::TT];
 #pragma unroll
@@ -240,6 +249,9 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_gemm_kernel(c
       const int token = m0 + loop.slab_row(i);
       loop.off_b[i] = (uint32_t)((int64_t)head_row(a, token < M ? token : M - 1) * a.ldb * 2) + loop.slab_col();
     }
+    const int64_t wr0 = r0 + loop.wr * C::RT * 32;
+    const int wm0 = m0 + loop.wt * C::TT * 32;
+    loop.active = wm0 < M;
     f32x16 acc[C::RT][C::TT];
 #pragma unroll
     for (int t = 0; t < C::RT; ++t)
@@ -248,12 +260,11 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_gemm_kernel(c
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
     loop.run(acc, 0, stages);
-    const int64_t wr0 = r0 + loop.wr * C::RT * 32;
-    const int wm0 = m0 + loop.wt * C::TT * 32;
-    if (wr0 < a.rows) head_statistics<C, PROBS, ENTROPY>(acc, a, M, wr0, wm0, a.part0 + rb * C::WR + loop.wr, loop.lane);
+    const bool results = loop.active && wr0 < a.rows;
+    if (results) head_statistics<C, PROBS, ENTROPY>(acc, a, M, wr0, wm0, a.part0 + rb * C::WR + loop.wr, loop.lane);
     if constexpr (PROBS) {
       lds_wait_barrier<0>();                       // nobody reads slabs any more
-      if (wr0 < a.rows)
+      if (results)
         store_tiles<C::TT, C::RT>(acc, 1.f, nullptr, a.p, a.ldp, M, (a.rows + 63) & ~(int64_t)63, wm0, wr0,
                                   reinterpret_cast<uint8_t*>(head_lds) + loop.wave * tile_out_bytes(C::RT), loop.lane);
     }
@@ -317,7 +328,9 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_sums_kernel(c
     for (int tt = 0; tt < C::TT; ++tt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
+  loop.active = m0 + loop.wt * C::TT * 32 < M;
   if (s1 > s0) loop.run(acc, s0, s1);
+  if (!loop.active) return;
   // partial sums stay in the registers' order: lane after lane, four rows of a token each
   f32x4* out = reinterpret_cast<f32x4*>(a.acc + u.part * a.slab) + ((int64_t)(u.mb * row_blocks + u.rb) * C::kWaves + loop.wave) * (C::RT * C::TT * 4 * 64) + loop.lane;
 #pragma unroll
@@ -341,42 +354,44 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_sums_kernel(c
   }
 }
 
-// slope = (1/T) [ (1 - p_t) W_t - sums e_scale ]; one workgroup per wave's part of a tile
+// slope = (1/T) [ (1 - p_t) W_t - sums e_scale ]; a workgroup takes one row tile of a wave's part of a tile, a wave of it one token tile
 template <class C>
 __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadArgs a, const uint16_t* W, int64_t ldw, int row_blocks, float inv_temperature,
                                                                      const float* rest, const float* e_scale, float* slope, int64_t ld_slope) {
   const int M = head_tokens(a);
-  const int wave = blockIdx.x % C::kWaves, tile = blockIdx.x / C::kWaves, rb = tile % row_blocks, mb = tile / row_blocks;
+  const int t = blockIdx.x % C::RT, wave = blockIdx.x / C::RT % C::kWaves, tile = blockIdx.x / (C::RT * C::kWaves), rb = tile % row_blocks, mb = tile / row_blocks;
   const int wr = wave % C::WR, wt = wave / C::WR, lane = threadIdx.x & 63, tt = threadIdx.x >> 6;
   const int token = mb * C::kTokens + (wt * C::TT + tt) * 32 + (lane & 31);
-  if (token >= M) return;
+  const int64_t h0 = (int64_t)rb * C::kRows + (wr * C::RT + t) * 32 + 4 * (lane >> 5);
+  if (token >= M || h0 >= a.rows) return;
   const int row = head_row(a, token);
-  const int64_t h0 = (int64_t)rb * C::kRows + wr * C::RT * 32 + 4 * (lane >> 5);
   const float r = rest[row] * inv_temperature, es = e_scale[row] * inv_temperature;
   const uint16_t* w = W + a.targets[row] * ldw;
   float* out = slope + (int64_t)row * ld_slope;
-  const f32x4* in = reinterpret_cast<const f32x4*>(a.acc) + ((int64_t)tile * C::kWaves + wave) * (C::RT * C::TT * 4 * 64) + lane;
+  const f32x4* in = reinterpret_cast<const f32x4*>(a.acc) + ((int64_t)tile * C::kWaves + wave) * (C::RT * C::TT * 4 * 64) + (tt * C::RT + t) * 4 * 64 + lane;
+  f32x4 s[4] = {};
+#pragma unroll 4
+  for (int z = 0; z < a.split; ++z)
 #pragma unroll
-  for (int t = 0; t < C::RT; ++t)
+    for (int q = 0; q < 4; ++q) s[q] += in[z * (a.slab / 4) + q * 64];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t h = h0 + t * 32 + 8 * q;
-      if (h >= a.rows) continue;                   // H is a multiple of 8: four rows are inside or beyond
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
-      for (int z = 0; z < a.split; ++z) s += in[z * (a.slab / 4) + (int64_t)((tt * C::RT + t) * 4 + q) * 64];
-      const u32x2 wv = *reinterpret_cast<const u32x2*>(w + h);
-      f32x4 o;
-      o[0] = bf16_bits_to_f32(wv[0] & 0xffffu) * r - s[0] * es;
-      o[1] = __uint_as_float(wv[0] & 0xffff0000u) * r - s[1] * es;
-      o[2] = bf16_bits_to_f32(wv[1] & 0xffffu) * r - s[2] * es;
-      o[3] = __uint_as_float(wv[1] & 0xffff0000u) * r - s[3] * es;
-      *reinterpret_cast<f32x4*>(out + h) = o;
-    }
+  for (int q = 0; q < 4; ++q) {
+    const int64_t h = h0 + 8 * q;
+    if (h >= a.rows) break;                      // H is a multiple of 8: four rows are inside or beyond
+    const u32x2 wv = *reinterpret_cast<const u32x2*>(w + h);
+    f32x4 o;
+    o[0] = bf16_bits_to_f32(wv[0] & 0xffffu) * r - s[q][0] * es;
+    o[1] = __uint_as_float(wv[0] & 0xffff0000u) * r - s[q][1] * es;
+    o[2] = bf16_bits_to_f32(wv[1] & 0xffffu) * r - s[q][2] * es;
+    o[3] = __uint_as_float(wv[1] & 0xffff0000u) * r - s[q][3] * es;
+    *reinterpret_cast<f32x4*>(out + h) = o;
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
 using Head256 = HeadCfg<4, 2, 2, 4, 3, 2>;       // 256 rows x 256 tokens
 using Head128 = HeadCfg<2, 2, 4, 2, 3, 2>;       // 256 rows x 128 tokens
+using Head320 = HeadCfg<5, 2, 2, 4, 2, 2>;       // 320 rows x 256 tokens: sums whose tiles of 256 would leave a round of workgroups half empty
 
 HeadGemmPlan plan_head_gemm(int64_t M) {
   if (M <= 64) return HeadGemmPlan{0, 0, 0};
@@ -394,23 +409,23 @@ static int allow_lds(K kernel, int bytes) {
 
 template <class C, bool PROBS, bool ENTROPY>
 static int launch_products(const HeadArgs& a, hipStream_t st) {
-  if (const int e = allow_lds(head_gemm_kernel<C, PROBS, ENTROPY>, C::kLds)) return e;
+  static_assert(C::kLdsProducts <= 160 * 1024, "LDS of a compute unit");
+  if (const int e = allow_lds(head_gemm_kernel<C, PROBS, ENTROPY>, C::kLdsProducts)) return e;
   const int row_blocks = (int)ceil_div(a.rows, C::kRows), per_xcd = (int)ceil_div(row_blocks, 8);
   int64_t grid = 8 * (int64_t)per_xcd * ceil_div(a.M, C::kTokens);
   if (a.flag && grid > 256) grid = 256;          // hardly ever anything to do: a few workgroups look at all tiles
-  head_gemm_kernel<C, PROBS, ENTROPY><<<dim3((unsigned)grid), dim3(C::kThreads), C::kLds, st>>>(a, row_blocks, per_xcd);
+  head_gemm_kernel<C, PROBS, ENTROPY><<<dim3((unsigned)grid), dim3(C::kThreads), C::kLdsProducts, st>>>(a, row_blocks, per_xcd);
   return launch_status();
 }
 template <class C>
 static int launch_sums(const HeadArgs& a, hipStream_t st) {
-  if (const int e = allow_lds(head_sums_kernel<C>, C::kLds)) return e;
+  if (const int e = allow_lds(head_sums_kernel<C>, C::kLdsSlabs)) return e;
   const int row_blocks = (int)ceil_div(a.rows, C::kRows), units = head_units_per_xcd(a.split, row_blocks, (int)ceil_div(a.M, C::kTokens));
-  head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLds, st>>>(a, row_blocks);
+  head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLdsSlabs, st>>>(a, row_blocks);
   return launch_status();
 }
 template <class C>
 static int launch_mode(HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st) {
-  if (mode == kSums) return launch_sums<C>(a, st);
   if (mode == kProbs) return entropy ? launch_products<C, true, true>(a, st) : launch_products<C, true, false>(a, st);
   return entropy ? launch_products<C, false, true>(a, st) : launch_products<C, false, false>(a, st);
 }
@@ -418,19 +433,25 @@ int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const H
   return p.tokens == Head256::kTokens ? launch_mode<Head256>(mode, entropy, a, st) : launch_mode<Head128>(mode, entropy, a, st);
 }
 
-// The split that costs least: rounds of units over the chip's 256 compute units, 0.9 us a stage, and the partial sums, which every piece
-// reads and writes at 5 TB/s.
+// Tile and split that cost least: rounds of units over the chip's 256 compute units at 1.6 us a stage of 256 x 256 (2 us to start one),
+// and the partial sums at 5 TB/s, which every piece reads and writes and the slopes read once.
 HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces) {
-  HeadSumsPlan q = {1, ceil_div(H, p.rows), ceil_div(M, p.tokens), 0};
-  const double tile_bytes = 4.0 * p.rows * p.tokens, stage_us = 0.9 * p.tokens / 256;
+  HeadSumsPlan q = {};
   double best = 1e30;
-  for (int split = 1; split <= 64 && split <= piece / 64; split *= 2) {
-    const int units = head_units_per_xcd(split, (int)q.row_blocks, (int)q.token_blocks);
-    const double us = (double)ceil_div(units, 32) * (double)ceil_div(piece / 64, split) * stage_us +
-                      (double)(q.row_blocks * q.token_blocks * split) * tile_bytes * (pieces > 1 ? 2 : 1) / 5e6;
-    if (us < best * 0.98) { best = us; q.split = split; }
+  for (int rows : {256, 320}) {
+    if (rows == 320 && p.tokens != 256) continue;
+    const int64_t row_blocks = ceil_div(H, rows), token_blocks = ceil_div(M, p.tokens);
+    const double tile_us = 4.0 * rows * p.tokens / 5e6, stage_us = 1.6 * (rows / 256.0) * (p.tokens / 256.0);
+    for (int split = 1; split <= 64 && (split == 1 || split <= piece / 64); split *= 2) {
+      const int64_t rounds = ceil_div(head_units_per_xcd(split, (int)row_blocks, (int)token_blocks), 32);
+      const double sums = (double)(row_blocks * token_blocks * split) * tile_us;
+      const double us = (double)pieces * ((double)rounds * (2.0 + (double)ceil_div(piece / 64, split) * stage_us) + sums * (pieces > 1 ? 2 : 1)) + sums;
+      if (us < best) {
+        best = us;
+        q = HeadSumsPlan{rows, split, (size_t)(row_blocks * token_blocks * split) * 4 * (size_t)(rows * p.tokens)};
+      }
+    }
   }
-  q.bytes = (size_t)(q.split * q.row_blocks * q.token_blocks) * 4 * (size_t)(p.rows * p.tokens);
   return q;
 }
 
@@ -438,14 +459,18 @@ template <class C>
 static int launch_slope(const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale, float* slope, int64_t ld_slope,
                         hipStream_t st) {
   const int row_blocks = (int)ceil_div(sums.rows, C::kRows);
-  head_tile_slope_kernel<C><<<dim3((unsigned)(row_blocks * ceil_div(sums.M, C::kTokens) * C::kWaves)), dim3(64 * C::TT), 0, st>>>(
+  head_tile_slope_kernel<C><<<dim3((unsigned)(row_blocks * ceil_div(sums.M, C::kTokens) * C::kWaves * C::RT)), dim3(64 * C::TT), 0, st>>>(
       sums, head.a, head.lda, row_blocks, inv_temperature, rest, e_scale, slope, ld_slope);
   return launch_status();
 }
-int launch_head_slope(const HeadGemmPlan& p, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale,
-                      float* slope, int64_t ld_slope, hipStream_t st) {
-  return p.tokens == Head256::kTokens ? launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-                                      : launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
+int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st) {
+  return p.tokens == 128 ? launch_sums<Head128>(a, st) : q.rows == 320 ? launch_sums<Head320>(a, st) : launch_sums<Head256>(a, st);
+}
+int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest,
+                      const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st) {
+  return p.tokens == 128 ? launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+       : q.rows == 320   ? launch_slope<Head320>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+                         : launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
 }
 
 }  // namespace qerl
