@@ -27,97 +27,6 @@ __device__ __forceinline__ void merge_sums(float& m, float& s, float& w, float m
   m = top;
 }
 
-// ---- a wave's 64 rows x 32 tokens, contraction split over the four waves of the workgroup -------------------------------
-// lane l of a 32 x 32 tile holds of token l % 32 the rows 8 q + 4 (l / 32) + 0..3 as elements 4 q .. 4 q + 3
-constexpr int kRowsPerBlock = 64, kTokensPerBlock = 32, kKWaves = 4;
-
-template <HeadMode MODE>
-__global__ __launch_bounds__(kKWaves * 64) void head_rows_kernel(const HeadArgs a) {
-  __shared__ float sums[kKWaves - 1][32][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n32 = lane & 31, kg = lane >> 5;
-  const int64_t r0 = (int64_t)blockIdx.x * kRowsPerBlock;
-  const int m0 = blockIdx.y * kTokensPerBlock;
-  if (MODE == kProbs && a.flag && !a.flag[blockIdx.y]) return;
-  const int token = m0 + n32 < a.M ? m0 + n32 : a.M - 1;
-  const int64_t ra = r0 + n32 < a.rows ? r0 + n32 : a.rows - 1, rb = r0 + 32 + n32 < a.rows ? r0 + 32 + n32 : a.rows - 1;
-  const uint16_t* pa = a.a + ra * a.lda;
-  const uint16_t* pb = a.a + rb * a.lda;
-  const uint16_t* px = a.b + (int64_t)token * a.ldb;
-  f32x16 acc[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
-  const int64_t steps = (a.k + 15) / 16, part = (int64_t)wave + (MODE == kSums ? (int64_t)blockIdx.z * kKWaves : 0), parts = (int64_t)kKWaves * (MODE == kSums ? a.split : 1);
-  const int64_t s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
-  auto load = [&](const uint16_t* p, int64_t s) {      // k is a multiple of 8: a chunk of eight is inside or beyond
-    const int64_t at = s * 16 + kg * 8;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(p + (at < a.k ? at : a.k - 8));
-    return __builtin_bit_cast(bf16x8, at < a.k ? v : u32x4{0u, 0u, 0u, 0u});
-  };
-  for (int64_t s = s0; s < s1; ++s) {
-    const bf16x8 x = load(px, s);
-    acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load(pa, s), x, acc[0], 0, 0, 0);
-    acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load(pb, s), x, acc[1], 0, 0, 0);
-  }
-  if (wave > 0) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) sums[wave - 1][i][lane] = acc[i >> 4][i & 15];
-  }
-  __syncthreads();
-  if (wave > 0) return;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) acc[i >> 4][i & 15] = (acc[i >> 4][i & 15] + sums[0][i][lane]) + (sums[1][i][lane] + sums[2][i][lane]);
-
-  const bool live = m0 + n32 < a.M;
-  if constexpr (MODE == kSums) {
-    if (!live) return;
-    const float alpha = a.first ? 0.f : exp2_fast(a.ref[token] == a.ref_next[token] ? 0.f : a.ref[token] - a.ref_next[token]);
-    float* out = a.acc + (int64_t)blockIdx.z * a.slab + (int64_t)token * a.ld_acc;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int64_t r = r0 + (i >> 4) * 32 + 8 * ((i >> 2) & 3) + 4 * kg + (i & 3);
-      if (r < a.rows) out[r] = a.first ? acc[i >> 4][i & 15] : alpha * out[r] + acc[i >> 4][i & 15];
-    }
-  } else {
-    const int64_t target = a.targets[token] - a.row0;
-    const float ref = MODE == kProbs ? (a.flag ? a.ref_next : a.ref)[token] : 0.f;
-    float top = kNegInf;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int64_t r = r0 + (i >> 4) * 32 + 8 * ((i >> 2) & 3) + 4 * kg + (i & 3);
-      float v = acc[i >> 4][i & 15] * a.scale;
-      if (r == target && live) a.target_logit[token] = v;
-      if (r == target || r >= a.rows) v = kNegInf;
-      acc[i >> 4][i & 15] = v;
-      top = fmaxf(top, v);
-    }
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float base = MODE == kProbs ? ref : top == kNegInf ? 0.f : top;
-    float sum = 0.f, weighted = 0.f;
-    uint32_t pr[16];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float d = acc[i >> 4][i & 15] - base, e = exp2_fast(d);
-      sum += e;
-      weighted += d == kNegInf ? 0.f : e * d;
-      if (MODE == kProbs) { if (i & 1) pr[i >> 1] |= f32_to_bf16_bits(e) << 16; else pr[i >> 1] = f32_to_bf16_bits(e); }
-    }
-    sum += __shfl_xor(sum, 32, 64);
-    weighted += __shfl_xor(weighted, 32, 64);
-    if (!live) return;
-    if (kg == 0) a.part[(int64_t)token * a.part_ld + a.part0 + blockIdx.x] = HeadPart{MODE == kProbs ? ref : top, sum, weighted, top};
-    if (MODE == kProbs) {
-      uint16_t* out = a.p + (int64_t)token * a.ldp;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int64_t r = r0 + (q >> 2) * 32 + 8 * (q & 3) + 4 * kg;
-        if (r < a.ldp) *reinterpret_cast<u32x2*>(out + r) = u32x2{pr[2 * q], pr[2 * q + 1]};
-      }
-    }
-  }
-}
-
 // Rows with a loss, in order: index[0 .. *count), and each row's place among them (-1: none)
 constexpr int kCompactThreads = 1024;
 __global__ __launch_bounds__(kCompactThreads) void head_compact_kernel(const int64_t* targets, int64_t V, int M, int* index, int* place, int* count) {
@@ -244,22 +153,6 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int 
   }
 }
 
-// slope = (1/T) [ (1 - p_t) W_t - sum_{v != t} p_v W_v ] from the rows kernel's sums
-__global__ __launch_bounds__(256) void head_slope_kernel(const HeadArgs a, const uint16_t* W, int64_t ldw, int64_t H, float inv_temperature, const float* rest,
-                                                         const float* e_scale, float* slope, int64_t ld_slope) {
-  const int token = blockIdx.x;
-  const int64_t target = a.targets[token];
-  if (target < 0 || target >= a.V) return;
-  float* out = slope + (int64_t)token * ld_slope;
-  const float r = rest[token], e = e_scale[token];
-  const uint16_t* w = W + target * ldw;
-  for (int64_t h = threadIdx.x; h < H; h += 256) {
-    float sum = 0.f;
-    for (int z = 0; z < a.split; ++z) sum += a.acc[z * a.slab + (int64_t)token * a.ld_acc + h];
-    out[h] = inv_temperature * (bf16_bits_to_f32(w[h]) * r - sum * e);
-  }
-}
-
 // dx = bf16(g slope)
 __global__ __launch_bounds__(256) void head_backward_kernel(const float* g, const float* slope, int64_t ld_slope, int M, int64_t H, uint16_t* dx, int64_t lddx) {
   const int token = blockIdx.y;
@@ -288,10 +181,10 @@ constexpr int64_t kTokenBlock = 8192;                     // tokens that are tak
 constexpr int64_t kPieceBytes = (int64_t)192 << 20;       // probabilities of a piece: they stay in the last-level cache until they are used
 
 struct HeadPlan {
-  HeadGemmPlan gemm;                                      // gemm.tokens == 0: the rows kernel
+  HeadGemmPlan gemm;
   HeadSumsPlan sums;
-  int64_t tokens, parts, part_rows, pieces, piece, flags; // tokens at a time; parts of a row; pieces and their rows (a multiple of 64), flags of a piece
-  int split;
+  bool compact;                                           // rows without a loss are left out of the products
+  int64_t tokens, parts, pieces, piece, flags;            // tokens at a time; parts of a row; pieces and their rows, flags of a piece
   size_t part, target, index, ref, flag, rest, p, acc, bytes;   // offsets
 };
 
@@ -310,39 +203,24 @@ static int64_t piece_blocks(int64_t blocks, int64_t most, int64_t token_blocks) 
 static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
   HeadPlan q = {};
   q.tokens = M < kTokenBlock ? M : kTokenBlock;
-  q.gemm = plan_head_gemm(q.tokens);
-  const bool gemm = q.gemm.tokens > 0;
-  const int64_t row_block = gemm ? q.gemm.rows : kRowsPerBlock, token_block = gemm ? q.gemm.tokens : kTokensPerBlock;
-  q.part_rows = gemm ? q.gemm.part_rows : kRowsPerBlock;
-  q.parts = ceil_div(V, q.part_rows);
-  q.pieces = 1;
-  q.piece = ceil_div(V, row_block) * row_block;
-  q.split = 1;
+  q.gemm = plan_head_gemm(q.tokens, gradient);
+  q.compact = q.tokens > 128;                             // fewer are one token block whatever they are
+  q.parts = ceil_div(V, q.gemm.part_rows);
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
   size_t at = 0;
   q.part = at; at += up((size_t)(q.tokens * q.parts) * sizeof(HeadPart));
   q.target = at; at += up((size_t)q.tokens * 4);
-  q.index = at; at += gemm ? up((size_t)(2 * q.tokens + 1) * 4) : 0;
+  q.index = at; at += q.compact ? up((size_t)(2 * q.tokens + 1) * 4) : 0;
   if (gradient) {
-    const int64_t token_blocks = ceil_div(q.tokens, token_block);
-    q.piece = piece_blocks(ceil_div(V, row_block), kPieceBytes / (2 * token_blocks * token_block * row_block), token_blocks) * row_block;
+    q.flags = ceil_div(q.tokens, q.gemm.tokens);
+    q.piece = piece_blocks(ceil_div(V, q.gemm.rows), kPieceBytes / (2 * q.flags * q.gemm.tokens * q.gemm.rows), q.flags) * q.gemm.rows;
     q.pieces = ceil_div(V, q.piece);
-    size_t acc = 0;
-    if (gemm) {
-      q.sums = plan_head_sums(q.gemm, q.tokens, H, q.piece, q.pieces);
-      q.split = q.sums.split;
-      acc = q.sums.bytes;
-    } else {
-      const int64_t groups = ceil_div(H, kRowsPerBlock) * token_blocks;
-      q.split = (int)(groups >= 512 ? 1 : ceil_div(512, groups) < 32 ? ceil_div(512, groups) : 32);
-      acc = (size_t)(q.split * q.tokens * H) * 4;
-    }
-    q.flags = token_blocks;
+    q.sums = plan_head_sums(q.gemm, q.tokens, H, q.piece, q.pieces);
     q.ref = at; at += up((size_t)(q.tokens * (q.pieces + 1)) * 4);
     q.flag = at; at += up((size_t)(q.flags * q.pieces) * 4);
     q.rest = at; at += up((size_t)(2 * q.tokens) * 4);
     q.p = at; at += up((size_t)(q.tokens * q.piece) * 2);
-    q.acc = at; at += up(acc);
+    q.acc = at; at += up(q.sums.bytes);
   }
   q.bytes = at;
   return q;
@@ -357,25 +235,14 @@ struct HeadCall {
   uint8_t* ws; size_t ws_bytes; hipStream_t st;
 };
 
-static int launch_rows(HeadMode mode, const HeadArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)ceil_div(a.rows, kRowsPerBlock), (unsigned)ceil_div(a.M, kTokensPerBlock), mode == kSums ? (unsigned)a.split : 1u), block(kKWaves * 64);
-  if (mode == kSums) head_rows_kernel<kSums><<<grid, block, 0, st>>>(a);
-  else if (mode == kProbs) head_rows_kernel<kProbs><<<grid, block, 0, st>>>(a);
-  else head_rows_kernel<kLogits><<<grid, block, 0, st>>>(a);
-  return launch_status();
-}
-
 static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t M) {
-  const bool gemm = q.gemm.tokens > 0;
+  const bool entropies = c.entropy != nullptr;
   HeadArgs a = {};
   a.a = c.W; a.lda = c.ldw; a.rows = c.V; a.b = c.x + m0 * c.ldx; a.ldb = c.ldx; a.k = c.H; a.M = (int)M;
   a.targets = c.targets + m0; a.V = c.V; a.scale = c.inv_temperature * 1.44269504088896341f;
   a.part = reinterpret_cast<HeadPart*>(c.ws + q.part); a.part_ld = q.parts; a.target_logit = reinterpret_cast<float*>(c.ws + q.target);
   int* place = nullptr;
-  auto launch = [&](HeadMode mode, const HeadArgs& args) {
-    return gemm ? launch_head_gemm(q.gemm, mode, c.entropy != nullptr, args, c.st) : launch_rows(mode, args, c.st);
-  };
-  if (gemm) {
+  if (q.compact) {
     int* index = reinterpret_cast<int*>(c.ws + q.index);
     place = index + q.tokens;
     head_compact_kernel<<<dim3(1), dim3(kCompactThreads), 0, c.st>>>(a.targets, c.V, (int)M, index, place, place + q.tokens);
@@ -385,7 +252,7 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
   float* lse = c.lse ? c.lse + m0 : nullptr;
   float* entropy = c.entropy ? c.entropy + m0 : nullptr;
   if (!c.slope) {
-    if (const int e = launch(kLogits, a)) return e;
+    if (const int e = launch_head_logits(q.gemm, entropies, a, c.st)) return e;
     head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.parts, place, nullptr, logprob, lse, entropy, nullptr, nullptr, nullptr, 0, 0);
     return launch_status();
   }
@@ -397,27 +264,25 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
   head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref, flags, (int)(q.flags * q.pieces));
   HeadArgs e = a;
   e.lda = ceil_div(c.V, 64) * 64; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
-  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.ld_acc = c.H; e.split = q.split;
-  e.slab = gemm ? ceil_div(c.H, q.sums.rows) * ceil_div(q.tokens, q.gemm.tokens) * q.sums.rows * q.gemm.tokens : q.tokens * c.H;
+  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.split = q.sums.split;
+  e.slab = ceil_div(c.H, q.sums.rows) * q.flags * q.sums.rows * q.gemm.tokens;
   for (int64_t i = 0; i < q.pieces; ++i) {
     const int64_t row0 = i * q.piece, rows = c.V - row0 < q.piece ? c.V - row0 : q.piece;
-    a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.part0 = (int)(row0 / q.part_rows);
+    a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.part0 = (int)(row0 / q.gemm.part_rows);
     a.p = reinterpret_cast<uint16_t*>(c.ws + q.p); a.ldp = q.piece;
     a.ref = ref + i * q.tokens; a.ref_next = ref + (i + 1) * q.tokens; a.flag = nullptr;
-    if (const int s = launch(kProbs, a)) return s;
-    head_check_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, (int)ceil_div(rows, q.part_rows), gemm ? q.gemm.tokens : kTokensPerBlock,
+    if (const int s = launch_head_probs(q.gemm, entropies, a, c.st)) return s;
+    head_check_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, (int)ceil_div(rows, q.gemm.part_rows), q.gemm.tokens,
                                                                               ref + (i + 1) * q.tokens, flags + i * q.flags);
     a.flag = flags + i * q.flags;
-    if (const int s = launch(kProbs, a)) return s;
+    if (const int s = launch_head_probs(q.gemm, entropies, a, c.st)) return s;
     e.a = c.Wt + row0; e.k = ceil_div(rows, 64) * 64; e.ref = a.ref; e.ref_next = a.ref_next; e.first = i == 0;
-    if (const int s = gemm ? launch_head_sums(q.gemm, q.sums, e, c.st) : launch_rows(kSums, e, c.st)) return s;
+    if (const int s = launch_head_sums(q.gemm, q.sums, e, c.st)) return s;
   }
   head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.parts, place, ref + q.pieces * q.tokens, logprob, lse, entropy, rest, e_scale, slope,
                                                                 c.ld_slope, c.H);
   a.a = c.W;
-  if (gemm) return launch_head_slope(q.gemm, q.sums, e, a, c.inv_temperature, rest, e_scale, slope, c.ld_slope, c.st);
-  head_slope_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(e, c.W, c.ldw, c.H, c.inv_temperature, rest, e_scale, slope, c.ld_slope);
-  return launch_status();
+  return launch_head_slope(q.gemm, q.sums, e, a, c.inv_temperature, rest, e_scale, slope, c.ld_slope, c.st);
 }
 
 static int run_head(const HeadCall& c, bool gradient) {

@@ -12,8 +12,6 @@ constexpr float kRaise = 60.f;                  // a logit this far (in powers o
 //   ref: what the sums are relative to, sum = sum_others 2^(s - ref), weighted = sum_others 2^(s - ref) (s - ref), top = max_others s
 struct HeadPart { float ref, sum, weighted, top; };
 
-enum HeadMode { kLogits, kProbs, kSums };
-
 struct HeadArgs {
   const uint16_t* a; int64_t lda, rows;         // row operand [rows, k]: W (rows = vocabulary) or its transpose (rows = hidden)
   const uint16_t* b; int64_t ldb;               // token operand [tokens, k]: x, or the piece's probabilities
@@ -28,20 +26,18 @@ struct HeadArgs {
   uint16_t* p; int64_t ldp;                     // probabilities 2^(s - ref) of the piece, 0 at the token's own row and beyond the vocabulary
   const float* ref; const float* ref_next;      // [tokens] the references of this piece and of the next (raised where a logit passed them by far)
   const int* flag;                              // [token blocks] which compute the piece again, with ref_next; null: first computation
-  float* acc; int64_t ld_acc; int64_t slab;     // sums E: [split][tokens][ld_acc] (rows kernel), [split][tiles][tile] (GEMM)
+  float* acc; int64_t slab;                     // sums E: [split][tiles][tile], `slab` floats per K-part
   int first;                                    // the sums start here
   int split;
 };
 __device__ __forceinline__ int head_tokens(const HeadArgs& a) { return a.count ? *a.count : a.M; }
 __device__ __forceinline__ int head_row(const HeadArgs& a, int token) { return a.index ? a.index[token] : token; }
 
-// the GEMM kernels (lm_head_gemm.hip)
-struct HeadGemmPlan {
-  int tokens;                                   // tokens of a tile: 128 or 256; 0: the GEMM does not take the call
-  int rows, part_rows;                          // vocabulary rows of a tile, of a part
-};
-HeadGemmPlan plan_head_gemm(int64_t M);
-int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st);      // kLogits, kProbs
+// the matrix kernels (lm_head_gemm.hip)
+struct HeadGemmPlan { int tokens, rows, part_rows; };   // tokens and vocabulary rows of a tile, rows of a part
+HeadGemmPlan plan_head_gemm(int64_t M, bool gradient);
+int launch_head_logits(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
+int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
 // the sums: rows of a tile, how K is split, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
 struct HeadSumsPlan { int rows, split; size_t bytes; };
 HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces);

@@ -1,4 +1,4 @@
-// The head's matrix products for more than a few tokens: logits of a piece of the vocabulary with their row statistics (and their
+// The head's matrix products: logits of a piece of the vocabulary with their row statistics (and their
 // probabilities, kept as bf16 for the piece only), and the sums E = P W over a piece.
 //
 // A workgroup of eight waves owns 256 rows x 256 tokens, a wave 128 x 64 of them.  Stages of 64 inputs: both operands go from memory to LDS
@@ -220,7 +220,7 @@ __device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], con
 }
 
 template <class C, bool PROBS, bool ENTROPY>
-__global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_gemm_kernel(const HeadArgs a, int row_blocks, int blocks_per_xcd) {
+__global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) void head_gemm_kernel(const HeadArgs a, int row_blocks, int blocks_per_xcd) {
   extern __shared__ __attribute__((aligned(256))) u32x4 head_lds[];
   HeadLoop<C> loop;
   loop.init(head_lds, threadIdx.x);
@@ -295,7 +295,7 @@ __host__ __device__ inline int head_units_per_xcd(int split, int row_blocks, int
 }
 
 template <class C>
-__global__ __launch_bounds__(C::kThreads, C::kWaves / 4) void head_sums_kernel(const HeadArgs a, int row_blocks) {
+__global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) void head_sums_kernel(const HeadArgs a, int row_blocks) {
   extern __shared__ __attribute__((aligned(256))) u32x4 head_lds[];
   HeadLoop<C> loop;
   loop.init(head_lds, threadIdx.x);
@@ -365,6 +365,7 @@ __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadA
   const int64_t h0 = (int64_t)rb * C::kRows + (wr * C::RT + t) * 32 + 4 * (lane >> 5);
   if (token >= M || h0 >= a.rows) return;
   const int row = head_row(a, token);
+  if (!a.index && (a.targets[row] < 0 || a.targets[row] >= a.V)) return;
   const float r = rest[row] * inv_temperature, es = e_scale[row] * inv_temperature;
   const uint16_t* w = W + a.targets[row] * ldw;
   float* out = slope + (int64_t)row * ld_slope;
@@ -389,13 +390,16 @@ __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadA
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
-using Head256 = HeadCfg<4, 2, 2, 4, 3, 2>;       // 256 rows x 256 tokens
+using Head32 = HeadCfg<2, 1, 2, 1, 4, 4>;        // 128 rows x 32 tokens, two workgroups of two waves per compute unit
+using Head64 = HeadCfg<2, 2, 2, 1, 3, 3>;        // 128 rows x 64 tokens
 using Head128 = HeadCfg<2, 2, 4, 2, 3, 2>;       // 256 rows x 128 tokens
+using Head256 = HeadCfg<4, 2, 2, 4, 3, 2>;       // 256 rows x 256 tokens
 using Head320 = HeadCfg<5, 2, 2, 4, 2, 2>;       // 320 rows x 256 tokens: sums whose tiles of 256 would leave a round of workgroups half empty
 
-HeadGemmPlan plan_head_gemm(int64_t M) {
-  if (M <= 64) return HeadGemmPlan{0, 0, 0};
-  // a token block of 128 leaves less unused where 256 would be half empty
+// The smallest tile that holds all tokens, so that few tokens stream the weights through small workgroups
+HeadGemmPlan plan_head_gemm(int64_t M, bool gradient) {
+  if (M <= 32 && !gradient) return HeadGemmPlan{Head32::kTokens, Head32::kRows, 32 * Head32::RT};
+  if (M <= 64) return HeadGemmPlan{Head64::kTokens, Head64::kRows, 32 * Head64::RT};
   if (M <= 128) return HeadGemmPlan{Head128::kTokens, Head128::kRows, 32 * Head128::RT};
   return HeadGemmPlan{Head256::kTokens, Head256::kRows, 32 * Head256::RT};
 }
@@ -424,26 +428,39 @@ static int launch_sums(const HeadArgs& a, hipStream_t st) {
   head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLdsSlabs, st>>>(a, row_blocks);
   return launch_status();
 }
-template <class C>
-static int launch_mode(HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st) {
-  if (mode == kProbs) return entropy ? launch_products<C, true, true>(a, st) : launch_products<C, true, false>(a, st);
-  return entropy ? launch_products<C, false, true>(a, st) : launch_products<C, false, false>(a, st);
+template <class C, bool PROBS>
+static int launch_mode(bool entropy, const HeadArgs& a, hipStream_t st) {
+  return entropy ? launch_products<C, PROBS, true>(a, st) : launch_products<C, PROBS, false>(a, st);
 }
-int launch_head_gemm(const HeadGemmPlan& p, HeadMode mode, bool entropy, const HeadArgs& a, hipStream_t st) {
-  return p.tokens == Head256::kTokens ? launch_mode<Head256>(mode, entropy, a, st) : launch_mode<Head128>(mode, entropy, a, st);
+int launch_head_logits(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st) {
+  switch (p.tokens) {
+    case 32: return launch_mode<Head32, false>(entropy, a, st);
+    case 64: return launch_mode<Head64, false>(entropy, a, st);
+    case 128: return launch_mode<Head128, false>(entropy, a, st);
+    default: return launch_mode<Head256, false>(entropy, a, st);
+  }
+}
+int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st) {
+  switch (p.tokens) {
+    case 64: return launch_mode<Head64, true>(entropy, a, st);
+    case 128: return launch_mode<Head128, true>(entropy, a, st);
+    default: return launch_mode<Head256, true>(entropy, a, st);
+  }
 }
 
-// Tile and split that cost least: rounds of units over the chip's 256 compute units at 1.6 us a stage of 256 x 256 (2 us to start one),
-// and the partial sums at 5 TB/s, which every piece reads and writes and the slopes read once.
+// Tile and split that cost least: rounds of units over the chip's compute units (two at a time for the smallest tile) at 1.6 us a stage of
+// 256 x 256 or what the row slab takes from memory (32 KB per unit at 6 TB/s over the chip: 1.4 us), 2 us to start a unit, and the partial
+// sums at 5 TB/s, which every piece reads and writes and the slopes read once.
 HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces) {
   HeadSumsPlan q = {};
   double best = 1e30;
-  for (int rows : {256, 320}) {
-    if (rows == 320 && p.tokens != 256) continue;
+  for (int rows : {128, 256, 320}) {
+    if (p.tokens == 256 ? rows == 128 : rows != p.rows) continue;
+    const int at_once = p.tokens == 64 ? 64 : 32;
     const int64_t row_blocks = ceil_div(H, rows), token_blocks = ceil_div(M, p.tokens);
-    const double tile_us = 4.0 * rows * p.tokens / 5e6, stage_us = 1.6 * (rows / 256.0) * (p.tokens / 256.0);
+    const double tile_us = 4.0 * rows * p.tokens / 5e6, stage_us = p.tokens == 256 ? 1.6 * rows / 256 : 1.4 * rows / 256 * at_once / 32;
     for (int split = 1; split <= 64 && (split == 1 || split <= piece / 64); split *= 2) {
-      const int64_t rounds = ceil_div(head_units_per_xcd(split, (int)row_blocks, (int)token_blocks), 32);
+      const int64_t rounds = ceil_div(head_units_per_xcd(split, (int)row_blocks, (int)token_blocks), at_once);
       const double sums = (double)(row_blocks * token_blocks * split) * tile_us;
       const double us = (double)pieces * ((double)rounds * (2.0 + (double)ceil_div(piece / 64, split) * stage_us) + sums * (pieces > 1 ? 2 : 1)) + sums;
       if (us < best) {
@@ -464,13 +481,17 @@ static int launch_slope(const HeadArgs& sums, const HeadArgs& head, float inv_te
   return launch_status();
 }
 int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st) {
-  return p.tokens == 128 ? launch_sums<Head128>(a, st) : q.rows == 320 ? launch_sums<Head320>(a, st) : launch_sums<Head256>(a, st);
+  return p.tokens == 64    ? launch_sums<Head64>(a, st)
+         : p.tokens == 128 ? launch_sums<Head128>(a, st)
+         : q.rows == 320   ? launch_sums<Head320>(a, st)
+                           : launch_sums<Head256>(a, st);
 }
 int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest,
                       const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st) {
-  return p.tokens == 128 ? launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-       : q.rows == 320   ? launch_slope<Head320>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-                         : launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
+  return p.tokens == 64    ? launch_slope<Head64>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+         : p.tokens == 128 ? launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+         : q.rows == 320   ? launch_slope<Head320>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+                           : launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
 }
 
 }  // namespace qerl
