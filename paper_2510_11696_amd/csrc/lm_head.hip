@@ -113,8 +113,17 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int 
   }
   const int token = place ? place[row] : row;
   float m = kNegInf, s = 0.f, w = 0.f;
-  for (int b = threadIdx.x; b < parts; b += 256) {
-    const HeadPart p = a.part[(int64_t)token * a.part_ld + b];
+  const HeadPart* part = a.part + (int64_t)token * a.part_ld;
+  int b = threadIdx.x;
+  for (; b + 3 * 256 < parts; b += 4 * 256) {    // four on their way at a time
+    HeadPart p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = part[b + 256 * i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) merge_sums(m, s, w, p[i].ref, p[i].sum, p[i].weighted);
+  }
+  for (; b < parts; b += 256) {
+    const HeadPart p = part[b];
     merge_sums(m, s, w, p.ref, p.sum, p.weighted);
   }
 #pragma unroll

@@ -47,6 +47,8 @@ struct HeadLoop {
     wr = wave % C::WR; wt = wave / C::WR;
     n32 = lane & 31; kg = lane >> 5;
   }
+  // row and byte inside it that a lane's request i fetches (rows further by whole requests have the same swizzle)
+  static_assert(C::kThreads % 128 == 0, "swizzle of later requests");
   __device__ __forceinline__ int slab_row(int i) const { return wave * 8 + (lane >> 3) + 8 * C::kWaves * i; }
   __device__ __forceinline__ uint32_t slab_col() const { return (uint32_t)(((lane & 7) ^ ((slab_row(0) >> 1) & 7)) * 16); }
   template <int N>
@@ -59,10 +61,11 @@ struct HeadLoop {
   // the last stage of a k that is no multiple of 64: through registers, zeros behind k (which is a multiple of 8)
   template <int N>
   __device__ __forceinline__ void copy_tail(const uint8_t* base, const uint32_t (&off)[N], int slab_chunks, int stage) {
-    const bool inside = (int64_t)stage * 128 + slab_col() < k * 2;
+    const int64_t at = (int64_t)stage * 128;
+    const bool inside = at + slab_col() < k * 2;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(base + off[i] + (inside ? (int64_t)stage * 128 : -(int64_t)slab_col()));
+      const u32x4 v = *reinterpret_cast<const u32x4*>(base + off[i] + (inside ? at : -(int64_t)slab_col()));
       lds[slab_chunks + i * C::kThreads + wave * 64 + lane] = inside ? v : u32x4{0u, 0u, 0u, 0u};
     }
   }
@@ -76,31 +79,33 @@ struct HeadLoop {
   }
   __device__ __forceinline__ bf16x8 frag(int chunk) const { return __builtin_bit_cast(bf16x8, lds[chunk]); }
 
-  __device__ __forceinline__ void run(f32x16 (&acc)[C::RT][C::TT], int s0, int s1) {
-    const int full = (int)(k >> 6);              // stages from here on take the tail's way
-    int next_a = s0, next_b = s0;                // next stages to fetch
-    int put_a = 0, put_b = 0;                    // their slots
-    auto fetch_a = [&] {
-      if (next_a < s1) {
-        if (next_a < full) request(base_a, off_a, put_a, next_a); else copy_tail(base_a, off_a, put_a, next_a);
-        ++next_a;
-        put_a = put_a + C::kSlabA == C::SA * C::kSlabA ? 0 : put_a + C::kSlabA;
-      }
-    };
-    auto fetch_b = [&] {
-      if (next_b < s1) {
-        const int at = C::SA * C::kSlabA + put_b;
-        if (next_b < full) request(base_b, off_b, at, next_b); else copy_tail(base_b, off_b, at, next_b);
-        ++next_b;
-        put_b = put_b + C::kSlabB == C::SB * C::kSlabB ? 0 : put_b + C::kSlabB;
-      }
-    };
-    // before the first stage: SB - 1 token slabs and SA - 1 row slabs, the last batch (token, row)
+  int s1, next_a, next_b, put_a, put_b;          // end of the stages, next ones to fetch and their slots
+  __device__ __forceinline__ void fetch_a() {
+    if (next_a >= s1) return;
+    if (next_a < (int)(k >> 6)) request(base_a, off_a, put_a, next_a); else copy_tail(base_a, off_a, put_a, next_a);
+    ++next_a;
+    put_a = put_a + C::kSlabA == C::SA * C::kSlabA ? 0 : put_a + C::kSlabA;
+  }
+  __device__ __forceinline__ void fetch_b() {
+    if (next_b >= s1) return;
+    const int at = C::SA * C::kSlabA + put_b;
+    if (next_b < (int)(k >> 6)) request(base_b, off_b, at, next_b); else copy_tail(base_b, off_b, at, next_b);
+    ++next_b;
+    put_b = put_b + C::kSlabB == C::SB * C::kSlabB ? 0 : put_b + C::kSlabB;
+  }
+  // Requests ahead of the first stage: SB - 1 token slabs and SA - 1 row slabs, the last batch (token, row).  Nobody reads LDS meanwhile.
+  __device__ __forceinline__ void start(int from, int to) {
+    next_a = next_b = from; s1 = to;
+    put_a = put_b = 0;
 #pragma unroll
     for (int i = 0; i < C::kDeep - 1; ++i) {
       if (i >= C::kDeep - C::SB) fetch_b();
       if (i >= C::kDeep - C::SA) fetch_a();
     }
+  }
+  // Stages from s0 on (as start was told), added to acc
+  __device__ __forceinline__ void run(f32x16 (&acc)[C::RT][C::TT], int s0) {
+    const int full = (int)(k >> 6);              // stages from here on take the tail's way
     auto meet = [&](int s) {                     // everybody has read stage s - 1, and stage s is in LDS
       if (s + C::kDeep - 2 < (s1 < full ? s1 : full)) lds_wait_barrier<C::kAhead>();
       else lds_wait_barrier<0>();
@@ -163,19 +168,19 @@ struct HeadLoop {
 
 // Row statistics of a wave's tile, from the products in acc; with PROBS acc becomes 2^(s - ref).
 // lane l holds of token 32 tt + l % 32 the rows 32 t + 8 q + 4 (l / 32) + 0..3 as elements 4 q .. 4 q + 3
+struct HeadLane { int own; float ref; };         // of a lane's token: its own row in the wave's tile, less 4 (l / 32) (or -1); its reference
 template <class C, bool PROBS, bool ENTROPY>
-__device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], const HeadArgs& a, int M, int64_t r0, int m0, int part, int lane) {
+__device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], const HeadArgs& a, const HeadLane (&of)[C::TT], int M, int64_t r0, int m0, int part,
+                                                int lane) {
   const int n32 = lane & 31, kg = lane >> 5;
   const float scale = a.scale;
 #pragma unroll
   for (int tt = 0; tt < C::TT; ++tt) {
     const int token = m0 + tt * 32 + n32;
     const bool live = token < M;
-    const int at = live ? token : M - 1;
-    const int64_t far = a.targets[head_row(a, at)] - a.row0 - r0;              // the token's own row, in the tile?
-    const bool mine = far >= 0 && far < 32 * C::RT && (((int)far >> 2) & 1) == kg;
+    const int own = of[tt].own;
+    const bool mine = own >= 0;
     if (__any(mine)) {
-      const int own = mine ? (int)far - 4 * kg : -1;
       float logit = 0.f;
 #pragma unroll
       for (int t = 0; t < C::RT; ++t)
@@ -200,7 +205,7 @@ __device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], con
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[t][tt][i]);
     top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;
-    const float ref = PROBS ? (a.flag ? a.ref_next : a.ref)[at] : top;
+    const float ref = PROBS ? of[tt].ref : top;
     const float base = PROBS ? ref : top == kNegInf ? 0.f : top;
     float sum[2] = {0.f, 0.f}, weighted[2] = {0.f, 0.f};
 #pragma unroll
@@ -227,14 +232,22 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
   loop.k = a.k;
   const int M = head_tokens(a), token_blocks = (M + C::kTokens - 1) / C::kTokens;
   const int stages = (int)((a.k + 63) >> 6), total = 8 * blocks_per_xcd * token_blocks;
-  for (int tile = blockIdx.x; tile < total; tile += gridDim.x) {
-    // workgroup ids go round-robin to the eight XCDs, each of which takes a contiguous eighth of the row blocks; four of them and all
-    // token blocks, rows first, make a group, so that what is in flight on an XCD shares its slabs
-    const int xcd = tile & 7, local = tile >> 3, group = local / (4 * token_blocks), in = local - group * 4 * token_blocks;
-    const int width = blocks_per_xcd - 4 * group < 4 ? blocks_per_xcd - 4 * group : 4;
-    const int mb = in / width, rb = xcd * blocks_per_xcd + 4 * group + in - mb * width;
-    if (rb >= row_blocks) continue;
-    if (PROBS && a.flag && !a.flag[mb]) continue;
+  int rb = 0, mb = 0;
+  HeadLane of[C::TT];
+  // The next tile from `tile` on that there is anything to do for; its operands.  Workgroup ids go round-robin to the eight XCDs, each of
+  // which takes a contiguous eighth of the row blocks; four of them and all token blocks, rows first, make a group, so that what is in
+  // flight on an XCD shares its slabs.
+  auto find = [&](int tile) {
+    for (; tile < total; tile += (int)gridDim.x) {
+      const int xcd = tile & 7, local = tile >> 3, group = local / (4 * token_blocks), in = local - group * 4 * token_blocks;
+      const int width = blocks_per_xcd - 4 * group < 4 ? blocks_per_xcd - 4 * group : 4;
+      mb = in / width;
+      rb = xcd * blocks_per_xcd + 4 * group + in - mb * width;
+      if (rb < row_blocks && !(PROBS && a.flag && !a.flag[mb])) break;
+    }
+    return tile;
+  };
+  auto prepare = [&] {
     const int64_t r0 = (int64_t)rb * C::kRows;
     const int m0 = mb * C::kTokens;
     loop.base_a = uniform_pointer(a.a + r0 * a.lda);
@@ -249,9 +262,21 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
       const int token = m0 + loop.slab_row(i);
       loop.off_b[i] = (uint32_t)((int64_t)head_row(a, token < M ? token : M - 1) * a.ldb * 2) + loop.slab_col();
     }
-    const int64_t wr0 = r0 + loop.wr * C::RT * 32;
     const int wm0 = m0 + loop.wt * C::TT * 32;
     loop.active = wm0 < M;
+#pragma unroll
+    for (int tt = 0; tt < C::TT; ++tt) {
+      const int token = wm0 + tt * 32 + loop.n32, at = token < M ? token : M - 1;
+      const int64_t far = a.targets[head_row(a, at)] - a.row0 - (r0 + loop.wr * C::RT * 32);
+      of[tt].own = far >= 0 && far < 32 * C::RT && (((int)far >> 2) & 1) == loop.kg ? (int)far - 4 * loop.kg : -1;
+      if constexpr (PROBS) of[tt].ref = (a.flag ? a.ref_next : a.ref)[at];
+    }
+    loop.start(0, stages);
+  };
+  int tile = find(blockIdx.x);
+  if (tile >= total) return;
+  prepare();
+  while (true) {
     f32x16 acc[C::RT][C::TT];
 #pragma unroll
     for (int t = 0; t < C::RT; ++t)
@@ -259,16 +284,32 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
       for (int tt = 0; tt < C::TT; ++tt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
-    loop.run(acc, 0, stages);
+    loop.run(acc, 0);
+    const int64_t wr0 = (int64_t)rb * C::kRows + loop.wr * C::RT * 32;
+    const int wm0 = mb * C::kTokens + loop.wt * C::TT * 32, part = a.part0 + rb * C::WR + loop.wr;
     const bool results = loop.active && wr0 < a.rows;
-    if (results) head_statistics<C, PROBS, ENTROPY>(acc, a, M, wr0, wm0, a.part0 + rb * C::WR + loop.wr, loop.lane);
+    tile = find(tile + (int)gridDim.x);
     if constexpr (PROBS) {
+      if (results) head_statistics<C, PROBS, ENTROPY>(acc, a, of, M, wr0, wm0, part, loop.lane);
       lds_wait_barrier<0>();                       // nobody reads slabs any more
       if (results)
         store_tiles<C::TT, C::RT>(acc, 1.f, nullptr, a.p, a.ldp, M, (a.rows + 63) & ~(int64_t)63, wm0, wr0,
                                   reinterpret_cast<uint8_t*>(head_lds) + loop.wave * tile_out_bytes(C::RT), loop.lane);
+      if (tile >= total) return;
+      lds_wait_barrier<0>();
+      prepare();
+    } else {
+      // the next tile's first slabs are on their way while this one's statistics are formed, which need no LDS
+      HeadLane now[C::TT];
+#pragma unroll
+      for (int tt = 0; tt < C::TT; ++tt) now[tt] = of[tt];
+      if (tile < total) {
+        lds_wait_barrier<0>();
+        prepare();
+      }
+      if (results) head_statistics<C, PROBS, ENTROPY>(acc, a, now, M, wr0, wm0, part, loop.lane);
+      if (tile >= total) return;
     }
-    if (tile + (int)gridDim.x < total) lds_wait_barrier<0>();                  // before the next tile's requests
   }
 }
 
@@ -302,7 +343,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
   loop.k = a.k;
   const int M = head_tokens(a), token_blocks = (M + C::kTokens - 1) / C::kTokens;
   if (M == 0) return;
-  const int stages = (int)(a.k >> 6);
+  const int stages = (int)((a.k + 63) >> 6);
   const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
   const HeadUnit u = head_unit(xcd, local, a.split, row_blocks, token_blocks);
   if (!u.any) return;
@@ -329,7 +370,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
   loop.active = m0 + loop.wt * C::TT * 32 < M;
-  if (s1 > s0) loop.run(acc, s0, s1);
+  if (s1 > s0) {
+    loop.start(s0, s1);
+    loop.run(acc, s0);
+  }
   if (!loop.active) return;
   // partial sums stay in the registers' order: lane after lane, four rows of a token each
   f32x4* out = reinterpret_cast<f32x4*>(a.acc + u.part * a.slab) + ((int64_t)(u.mb * row_blocks + u.rb) * C::kWaves + loop.wave) * (C::RT * C::TT * 4 * 64) + loop.lane;
@@ -417,7 +461,9 @@ static int launch_products(const HeadArgs& a, hipStream_t st) {
   if (const int e = allow_lds(head_gemm_kernel<C, PROBS, ENTROPY>, C::kLdsProducts)) return e;
   const int row_blocks = (int)ceil_div(a.rows, C::kRows), per_xcd = (int)ceil_div(row_blocks, 8);
   int64_t grid = 8 * (int64_t)per_xcd * ceil_div(a.M, C::kTokens);
-  if (a.flag && grid > 256) grid = 256;          // hardly ever anything to do: a few workgroups look at all tiles
+  // as many workgroups as fit at once where one goes on to its next tile while it finishes the last, or where hardly ever one has anything to do
+  const int64_t at_once = 256 * (160 * 1024 / C::kLdsProducts);
+  if ((!PROBS || a.flag) && grid > at_once) grid = at_once;
   head_gemm_kernel<C, PROBS, ENTROPY><<<dim3((unsigned)grid), dim3(C::kThreads), C::kLdsProducts, st>>>(a, row_blocks, per_xcd);
   return launch_status();
 }
