@@ -224,7 +224,7 @@ static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
     q.flags = ceil_div(q.tokens, q.gemm.tokens);
     q.piece = piece_blocks(ceil_div(V, q.gemm.rows), kPieceBytes / (2 * q.flags * q.gemm.tokens * q.gemm.rows), q.flags) * q.gemm.rows;
     q.pieces = ceil_div(V, q.piece);
-    q.sums = plan_head_sums(q.gemm, q.tokens, H, q.piece, q.pieces);
+    q.sums = plan_head_sums(q.gemm, q.tokens, H, q.piece);
     q.ref = at; at += up((size_t)(q.tokens * (q.pieces + 1)) * 4);
     q.flag = at; at += up((size_t)(q.flags * q.pieces) * 4);
     q.rest = at; at += up((size_t)(2 * q.tokens) * 4);
@@ -273,8 +273,7 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
   head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref, flags, (int)(q.flags * q.pieces));
   HeadArgs e = a;
   e.lda = ceil_div(c.V, 64) * 64; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
-  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.split = q.sums.split;
-  e.slab = ceil_div(c.H, q.sums.rows) * q.flags * q.sums.rows * q.gemm.tokens;
+  e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.piece_stages = (int)(q.piece / 64);
   for (int64_t i = 0; i < q.pieces; ++i) {
     const int64_t row0 = i * q.piece, rows = c.V - row0 < q.piece ? c.V - row0 : q.piece;
     a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.part0 = (int)(row0 / q.gemm.part_rows);

@@ -26,9 +26,9 @@ struct HeadArgs {
   uint16_t* p; int64_t ldp;                     // probabilities 2^(s - ref) of the piece, 0 at the token's own row and beyond the vocabulary
   const float* ref; const float* ref_next;      // [tokens] the references of this piece and of the next (raised where a logit passed them by far)
   const int* flag;                              // [token blocks] which compute the piece again, with ref_next; null: first computation
-  float* acc; int64_t slab;                     // sums E: [split][tiles][tile], `slab` floats per K-part
+  float* acc;                                   // sums E: [K-part][token block][row block][tile]
   int first;                                    // the sums start here
-  int split;
+  int piece_stages;                             // of 64 rows in a whole piece
 };
 __device__ __forceinline__ int head_tokens(const HeadArgs& a) { return a.count ? *a.count : a.M; }
 __device__ __forceinline__ int head_row(const HeadArgs& a, int token) { return a.index ? a.index[token] : token; }
@@ -38,9 +38,9 @@ struct HeadGemmPlan { int tokens, rows, part_rows; };   // tokens and vocabulary
 HeadGemmPlan plan_head_gemm(int64_t M, bool gradient);
 int launch_head_logits(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
 int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
-// the sums: rows of a tile, how K is split, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
-struct HeadSumsPlan { int rows, split; size_t bytes; };
-HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces);
+// the sums: rows of a tile, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
+struct HeadSumsPlan { int rows; size_t bytes; };
+HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece);
 int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st);
 int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest,
                       const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st);

@@ -317,22 +317,44 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
 // Unit u of `split` x tiles: which K-part, row block and token block.  The eight XCDs share the K-parts out (several of them to a part
 // where there are fewer than eight), and inside a part the tiles, so that an XCD's caches see few slabs.
 struct HeadUnit { int part, rb, mb; bool any; };
-__device__ __forceinline__ HeadUnit head_unit(int xcd, int local, int split, int row_blocks, int token_blocks) {
-  const int tiles = row_blocks * token_blocks;
-  if (split >= 8) {
-    const int turn = local / tiles, in = local - turn * tiles, part = turn * 8 + xcd;
-    return HeadUnit{part, in % row_blocks, in / row_blocks, part < split};
-  }
-  const int xs = 8 / split, part = xcd / xs, x = xcd % xs;             // xs XCDs take the tiles of a part: 1, 2 x 1, 2 x 2 or 4 x 2 of rows x tokens
-  const int xr = xs >= 8 ? 4 : xs >= 2 ? 2 : 1, xt = xs / xr;
-  const int nr = (row_blocks + xr - 1) / xr, nt = (token_blocks + xt - 1) / xt;
-  const int rb = (x % xr) * nr + local % nr, mb = (x / xr) * nt + local / nr;
-  return HeadUnit{part, rb, mb, local < nr * nt && local % nr + (x % xr) * nr < row_blocks && mb < token_blocks};
+struct HeadShare { int rows, tokens; };          // log2 of how many ways 2^(3 - log_split) XCDs share the row blocks and the token blocks of a part
+__host__ __device__ inline HeadShare head_share(int log_split) {
+  const int rows = log_split == 0 ? 2 : log_split == 3 ? 0 : 1;
+  return HeadShare{rows, 3 - log_split - rows};
 }
-__host__ __device__ inline int head_units_per_xcd(int split, int row_blocks, int token_blocks) {
-  if (split >= 8) return (split + 7) / 8 * row_blocks * token_blocks;
-  const int xs = 8 / split, xr = xs >= 8 ? 4 : xs >= 2 ? 2 : 1, xt = xs / xr;
-  return ((row_blocks + xr - 1) / xr) * ((token_blocks + xt - 1) / xt);
+__device__ __forceinline__ HeadUnit head_unit(int xcd, int local, int log_split, int row_blocks, int token_blocks) {
+  if (log_split >= 3) {
+    const int tiles = row_blocks * token_blocks, turn = local / tiles, in = local - turn * tiles, part = turn * 8 + xcd;
+    return HeadUnit{part, in % row_blocks, in / row_blocks, part < 1 << log_split};
+  }
+  const HeadShare h = head_share(log_split);
+  const int part = xcd >> (3 - log_split), x = xcd & ((8 >> log_split) - 1);
+  const int nr = (row_blocks + (1 << h.rows) - 1) >> h.rows, nt = (token_blocks + (1 << h.tokens) - 1) >> h.tokens;
+  const int r = local % nr, rb = (x & ((1 << h.rows) - 1)) * nr + r, mb = (x >> h.rows) * nt + local / nr;
+  return HeadUnit{part, rb, mb, local < nr * nt && rb < row_blocks && mb < token_blocks};
+}
+__host__ __device__ inline int head_units_per_xcd(int log_split, int row_blocks, int token_blocks) {
+  if (log_split >= 3) return (row_blocks * token_blocks) << (log_split - 3);
+  const HeadShare h = head_share(log_split);
+  return ((row_blocks + (1 << h.rows) - 1) >> h.rows) * ((token_blocks + (1 << h.tokens) - 1) >> h.tokens);
+}
+
+// log2 of how many parts K is split into: rounds of units over the chip's compute units (two at a time for the smallest tile) at 1.6 us a
+// stage of 256 x 256 or what the row slab takes from memory (32 KB per unit at 6 TB/s over the chip: 1.4 us), 2 us to start a unit, and the
+// partial sums at 5 TB/s, which every piece reads and writes.  Whole nanoseconds: the host sizes the sums by the same function that the
+// kernels evaluate for the rows that have a loss.
+struct HeadSplit { int log_split; int64_t ns; };
+template <int ROWS, int TOKENS>
+__host__ __device__ inline HeadSplit head_split(int row_blocks, int token_blocks, int stages) {
+  constexpr int kAtOnce = TOKENS == 64 ? 64 : 32, kStage = TOKENS == 256 ? 1600 * ROWS / 256 : 1400 * ROWS / 256 * kAtOnce / 32,
+                kTile = 2 * ROWS * TOKENS * 4 / 5000;
+  HeadSplit best = {0, INT64_MAX};
+  for (int l = 0; l <= 6 && (l == 0 || 1 << l <= stages); ++l) {
+    const int rounds = (head_units_per_xcd(l, row_blocks, token_blocks) + kAtOnce - 1) / kAtOnce;
+    const int64_t ns = rounds * (2000 + (int64_t)((stages + (1 << l) - 1) >> l) * kStage) + ((int64_t)(row_blocks * token_blocks) << l) * kTile;
+    if (ns < best.ns) best = HeadSplit{l, ns};
+  }
+  return best;
 }
 
 template <class C>
@@ -345,9 +367,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
   if (M == 0) return;
   const int stages = (int)((a.k + 63) >> 6);
   const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
-  const HeadUnit u = head_unit(xcd, local, a.split, row_blocks, token_blocks);
+  const int split = head_split<C::kRows, C::kTokens>(row_blocks, token_blocks, a.piece_stages).log_split;
+  const HeadUnit u = head_unit(xcd, local, split, row_blocks, token_blocks);
   if (!u.any) return;
-  const int s0 = (int)((int64_t)stages * u.part / a.split), s1 = (int)((int64_t)stages * (u.part + 1) / a.split);
+  const int s0 = (int)((int64_t)stages * u.part >> split), s1 = (int)((int64_t)stages * (u.part + 1) >> split);
   const int64_t r0 = (int64_t)u.rb * C::kRows;
   const int m0 = u.mb * C::kTokens;
   loop.base_a = uniform_pointer(a.a + r0 * a.lda);
@@ -376,7 +399,8 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
   }
   if (!loop.active) return;
   // partial sums stay in the registers' order: lane after lane, four rows of a token each
-  f32x4* out = reinterpret_cast<f32x4*>(a.acc + u.part * a.slab) + ((int64_t)(u.mb * row_blocks + u.rb) * C::kWaves + loop.wave) * (C::RT * C::TT * 4 * 64) + loop.lane;
+  f32x4* out = reinterpret_cast<f32x4*>(a.acc) + (((int64_t)u.part * token_blocks + u.mb) * row_blocks + u.rb) * (C::kRows * C::kTokens / 4) +
+               loop.wave * (C::RT * C::TT * 4 * 64) + loop.lane;
 #pragma unroll
   for (int tt = 0; tt < C::TT; ++tt) {
     int token = m0 + (loop.wt * C::TT + tt) * 32 + loop.n32;
@@ -413,12 +437,14 @@ __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadA
   const float r = rest[row] * inv_temperature, es = e_scale[row] * inv_temperature;
   const uint16_t* w = W + a.targets[row] * ldw;
   float* out = slope + (int64_t)row * ld_slope;
-  const f32x4* in = reinterpret_cast<const f32x4*>(a.acc) + ((int64_t)tile * C::kWaves + wave) * (C::RT * C::TT * 4 * 64) + (tt * C::RT + t) * 4 * 64 + lane;
+  const int token_blocks = (M + C::kTokens - 1) / C::kTokens, split = 1 << head_split<C::kRows, C::kTokens>(row_blocks, token_blocks, a.piece_stages).log_split;
+  const f32x4* in = reinterpret_cast<const f32x4*>(a.acc) + (int64_t)tile * (C::kRows * C::kTokens / 4) + wave * (C::RT * C::TT * 4 * 64) + (tt * C::RT + t) * 4 * 64 + lane;
+  const int64_t slab = (int64_t)token_blocks * row_blocks * (C::kRows * C::kTokens / 4);
   f32x4 s[4] = {};
 #pragma unroll 4
-  for (int z = 0; z < a.split; ++z)
+  for (int z = 0; z < split; ++z)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) s[q] += in[z * (a.slab / 4) + q * 64];
+    for (int q = 0; q < 4; ++q) s[q] += in[z * slab + q * 64];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int64_t h = h0 + 8 * q;
@@ -470,7 +496,12 @@ static int launch_products(const HeadArgs& a, hipStream_t st) {
 template <class C>
 static int launch_sums(const HeadArgs& a, hipStream_t st) {
   if (const int e = allow_lds(head_sums_kernel<C>, C::kLdsSlabs)) return e;
-  const int row_blocks = (int)ceil_div(a.rows, C::kRows), units = head_units_per_xcd(a.split, row_blocks, (int)ceil_div(a.M, C::kTokens));
+  const int row_blocks = (int)ceil_div(a.rows, C::kRows), token_blocks = (int)ceil_div(a.M, C::kTokens);
+  int units = 0;                                 // of an XCD, at most, whatever number of rows has a loss
+  for (int tb = a.count ? 1 : token_blocks; tb <= token_blocks; ++tb) {
+    const int n = head_units_per_xcd(head_split<C::kRows, C::kTokens>(row_blocks, tb, a.piece_stages).log_split, row_blocks, tb);
+    units = n > units ? n : units;
+  }
   head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLdsSlabs, st>>>(a, row_blocks);
   return launch_status();
 }
@@ -494,26 +525,27 @@ int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hi
   }
 }
 
-// Tile and split that cost least: rounds of units over the chip's compute units (two at a time for the smallest tile) at 1.6 us a stage of
-// 256 x 256 or what the row slab takes from memory (32 KB per unit at 6 TB/s over the chip: 1.4 us), 2 us to start a unit, and the partial
-// sums at 5 TB/s, which every piece reads and writes and the slopes read once.
-HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece, int64_t pieces) {
+// The tile that costs least, and what its partial sums take for up to M rows with a loss
+template <class C>
+static void consider_sums(HeadSumsPlan& q, int64_t& best, int64_t M, int64_t H, int64_t piece) {
+  const int token_blocks = (int)ceil_div(M, C::kTokens), row_blocks = (int)ceil_div(H, C::kRows), stages = (int)(piece / 64);
+  const int64_t ns = head_split<C::kRows, C::kTokens>(row_blocks, token_blocks, stages).ns;
+  if (ns >= best) return;
+  best = ns;
+  q = HeadSumsPlan{C::kRows, 0};
+  for (int tb = 1; tb <= token_blocks; ++tb) {
+    const size_t bytes = ((size_t)(row_blocks * tb) << head_split<C::kRows, C::kTokens>(row_blocks, tb, stages).log_split) * 4 * C::kRows * C::kTokens;
+    q.bytes = bytes > q.bytes ? bytes : q.bytes;
+  }
+}
+HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece) {
   HeadSumsPlan q = {};
-  double best = 1e30;
-  for (int rows : {128, 256, 320}) {
-    if (p.tokens == 256 ? rows == 128 : rows != p.rows) continue;
-    const int at_once = p.tokens == 64 ? 64 : 32;
-    const int64_t row_blocks = ceil_div(H, rows), token_blocks = ceil_div(M, p.tokens);
-    const double tile_us = 4.0 * rows * p.tokens / 5e6, stage_us = p.tokens == 256 ? 1.6 * rows / 256 : 1.4 * rows / 256 * at_once / 32;
-    for (int split = 1; split <= 64 && (split == 1 || split <= piece / 64); split *= 2) {
-      const int64_t rounds = ceil_div(head_units_per_xcd(split, (int)row_blocks, (int)token_blocks), at_once);
-      const double sums = (double)(row_blocks * token_blocks * split) * tile_us;
-      const double us = (double)pieces * ((double)rounds * (2.0 + (double)ceil_div(piece / 64, split) * stage_us) + sums * (pieces > 1 ? 2 : 1)) + sums;
-      if (us < best) {
-        best = us;
-        q = HeadSumsPlan{rows, split, (size_t)(row_blocks * token_blocks * split) * 4 * (size_t)(rows * p.tokens)};
-      }
-    }
+  int64_t best = INT64_MAX;
+  if (p.tokens == 64) consider_sums<Head64>(q, best, M, H, piece);
+  else if (p.tokens == 128) consider_sums<Head128>(q, best, M, H, piece);
+  else {
+    consider_sums<Head256>(q, best, M, H, piece);
+    consider_sums<Head320>(q, best, M, H, piece);
   }
   return q;
 }
