@@ -9,7 +9,6 @@
 // Operand layout in LDS: rows of 64 inputs as eight 16-byte chunks, chunk c of row r at r * 8 + (c ^ ((r >> 1) & 7)).
 #include "lm_head.hpp"
 #include "lds_dma.hpp"
-#include "tile_out.hpp"
 
 namespace qerl {
 
@@ -21,9 +20,8 @@ struct HeadCfg {
   static constexpr int kSlabA = kRows * 8, kSlabB = kTokens * 8;                // 16-byte chunks
   static constexpr int IA = kSlabA / kThreads, IB = kSlabB / kThreads;          // requests per wave and stage
   static_assert(IA * kThreads == kSlabA && IB * kThreads == kSlabB, "whole requests");
-  static constexpr int kLdsSlabs = (SA * kSlabA + SB * kSlabB) * 16, kLdsOut = kWaves * tile_out_bytes(RT);
-  static constexpr int kLdsProducts = kLdsSlabs > kLdsOut ? kLdsSlabs : kLdsOut;
-  static_assert(kLdsSlabs <= 160 * 1024, "LDS of a compute unit");
+  static constexpr int kLds = (SA * kSlabA + SB * kSlabB) * 16;
+  static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
   // requests that may be outstanding when stage s + 1 is needed: those behind its own, batches being (token slab, row slab)
   static constexpr int kAfterB = IA + (SB - 2) * (IA + IB), kAfterA = (SA - 2) * (IA + IB);
   static constexpr int kAhead = kAfterA < kAfterB ? kAfterA : kAfterB;
@@ -224,6 +222,28 @@ __device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], con
   }
 }
 
+// The probabilities in acc as bf16 to p, row-major by token: a lane and its partner 32 further hold rows 4 kg + 0..3 of each eight; two
+// swaps per sixteen rows give each of them eight in a row, 16 bytes.
+template <class C>
+__device__ __forceinline__ void store_probs(const f32x16 (&acc)[C::RT][C::TT], const HeadArgs& a, int M, int64_t r0, int m0, int lane) {
+  const int n32 = lane & 31, kg = lane >> 5;
+  const int64_t end = (a.rows + 63) & ~(int64_t)63;
+#pragma unroll
+  for (int tt = 0; tt < C::TT; ++tt) {
+    const int token = m0 + tt * 32 + n32;
+    uint16_t* out = a.p + (int64_t)token * a.ldp + r0 + 8 * kg;
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const f32x16& v = acc[t][tt];
+        const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16x2(v[8 * g], v[8 * g + 1]), pack_bf16x2(v[8 * g + 4], v[8 * g + 5]), false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16x2(v[8 * g + 2], v[8 * g + 3]), pack_bf16x2(v[8 * g + 6], v[8 * g + 7]), false, false);
+        if (token < M && r0 + t * 32 + 16 * g < end) *reinterpret_cast<u32x4*>(out + t * 32 + 16 * g) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      }
+  }
+}
+
 template <class C, bool PROBS, bool ENTROPY>
 __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) void head_gemm_kernel(const HeadArgs a, int row_blocks, int blocks_per_xcd) {
   extern __shared__ __attribute__((aligned(256))) u32x4 head_lds[];
@@ -289,27 +309,19 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
     const int wm0 = mb * C::kTokens + loop.wt * C::TT * 32, part = a.part0 + rb * C::WR + loop.wr;
     const bool results = loop.active && wr0 < a.rows;
     tile = find(tile + (int)gridDim.x);
-    if constexpr (PROBS) {
-      if (results) head_statistics<C, PROBS, ENTROPY>(acc, a, of, M, wr0, wm0, part, loop.lane);
-      lds_wait_barrier<0>();                       // nobody reads slabs any more
-      if (results)
-        store_tiles<C::TT, C::RT>(acc, 1.f, nullptr, a.p, a.ldp, M, (a.rows + 63) & ~(int64_t)63, wm0, wr0,
-                                  reinterpret_cast<uint8_t*>(head_lds) + loop.wave * tile_out_bytes(C::RT), loop.lane);
-      if (tile >= total) return;
+    // the next tile's first slabs are on their way while this one's statistics are formed, which need no LDS
+    HeadLane now[C::TT];
+#pragma unroll
+    for (int tt = 0; tt < C::TT; ++tt) now[tt] = of[tt];
+    if (tile < total) {
       lds_wait_barrier<0>();
       prepare();
-    } else {
-      // the next tile's first slabs are on their way while this one's statistics are formed, which need no LDS
-      HeadLane now[C::TT];
-#pragma unroll
-      for (int tt = 0; tt < C::TT; ++tt) now[tt] = of[tt];
-      if (tile < total) {
-        lds_wait_barrier<0>();
-        prepare();
-      }
-      if (results) head_statistics<C, PROBS, ENTROPY>(acc, a, now, M, wr0, wm0, part, loop.lane);
-      if (tile >= total) return;
     }
+    if (results) {
+      head_statistics<C, PROBS, ENTROPY>(acc, a, now, M, wr0, wm0, part, loop.lane);
+      if constexpr (PROBS) store_probs<C>(acc, a, M, wr0, wm0, loop.lane);
+    }
+    if (tile >= total) return;
   }
 }
 
@@ -483,26 +495,25 @@ static int allow_lds(K kernel, int bytes) {
 
 template <class C, bool PROBS, bool ENTROPY>
 static int launch_products(const HeadArgs& a, hipStream_t st) {
-  static_assert(C::kLdsProducts <= 160 * 1024, "LDS of a compute unit");
-  if (const int e = allow_lds(head_gemm_kernel<C, PROBS, ENTROPY>, C::kLdsProducts)) return e;
+  if (const int e = allow_lds(head_gemm_kernel<C, PROBS, ENTROPY>, C::kLds)) return e;
   const int row_blocks = (int)ceil_div(a.rows, C::kRows), per_xcd = (int)ceil_div(row_blocks, 8);
   int64_t grid = 8 * (int64_t)per_xcd * ceil_div(a.M, C::kTokens);
-  // as many workgroups as fit at once where one goes on to its next tile while it finishes the last, or where hardly ever one has anything to do
-  const int64_t at_once = 256 * (160 * 1024 / C::kLdsProducts);
-  if ((!PROBS || a.flag) && grid > at_once) grid = at_once;
-  head_gemm_kernel<C, PROBS, ENTROPY><<<dim3((unsigned)grid), dim3(C::kThreads), C::kLdsProducts, st>>>(a, row_blocks, per_xcd);
+  // as many workgroups as fit at once: each goes on to its next tile while it finishes the last
+  const int64_t at_once = 256 * (160 * 1024 / C::kLds);
+  if (grid > at_once) grid = at_once;
+  head_gemm_kernel<C, PROBS, ENTROPY><<<dim3((unsigned)grid), dim3(C::kThreads), C::kLds, st>>>(a, row_blocks, per_xcd);
   return launch_status();
 }
 template <class C>
 static int launch_sums(const HeadArgs& a, hipStream_t st) {
-  if (const int e = allow_lds(head_sums_kernel<C>, C::kLdsSlabs)) return e;
+  if (const int e = allow_lds(head_sums_kernel<C>, C::kLds)) return e;
   const int row_blocks = (int)ceil_div(a.rows, C::kRows), token_blocks = (int)ceil_div(a.M, C::kTokens);
   int units = 0;                                 // of an XCD, at most, whatever number of rows has a loss
   for (int tb = a.count ? 1 : token_blocks; tb <= token_blocks; ++tb) {
     const int n = head_units_per_xcd(head_split<C::kRows, C::kTokens>(row_blocks, tb, a.piece_stages).log_split, row_blocks, tb);
     units = n > units ? n : units;
   }
-  head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLdsSlabs, st>>>(a, row_blocks);
+  head_sums_kernel<C><<<dim3((unsigned)(8 * units)), dim3(C::kThreads), C::kLds, st>>>(a, row_blocks);
   return launch_status();
 }
 template <class C, bool PROBS>
