@@ -125,32 +125,30 @@ struct HeadLoop {
     for (int t = 0; t < C::TT; ++t) fb[t] = frag(chunk_b(slot_b, 0, t));
 #pragma unroll
     for (int t = 0; t < C::RT; ++t) fa[t] = frag(chunk_a(slot_a, 0, t));
-    for (int s = s0; s < s1; ++s) {
-      const int after_a = slot_a + C::kSlabA == C::SA * C::kSlabA ? 0 : slot_a + C::kSlabA;
-      const int after_b = slot_b + C::kSlabB == C::SB * C::kSlabB ? 0 : slot_b + C::kSlabB;
+    // One step's matrix instructions, the next step's fragments read between them, `between(i)` behind instruction i
+    auto step = [&](int ca, int cb, int jn, auto between) {
+      bf16x8 na[C::RT], nb[C::TT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (j == 3 && s + 1 < s1) {
-          __builtin_amdgcn_sched_barrier(0);
-          meet(s + 1);
-          fetch_b();
-          fetch_a();
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        const int ca = j < 3 ? slot_a : after_a, cb = j < 3 ? slot_b : after_b, jn = (j + 1) & 3;
-        bf16x8 na[C::RT], nb[C::TT];
+      for (int i = 0; i < C::RT * C::TT; ++i) {
+        const int t = i / C::TT, tt = i % C::TT;
+        acc[t][tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[t], fb[tt], acc[t][tt], 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < C::TT; ++t) nb[t] = frag(chunk_b(cb, jn, t));     // behind the last stage: whatever the slot holds, not used
+        for (int r = i * (C::RT + C::TT) / (C::RT * C::TT); r < (i + 1) * (C::RT + C::TT) / (C::RT * C::TT); ++r)
+          if (r < C::TT) nb[r] = frag(chunk_b(cb, jn, r)); else na[r - C::TT] = frag(chunk_a(ca, jn, r - C::TT));
+        between(i);
+      }
 #pragma unroll
-        for (int t = 0; t < C::RT; ++t) na[t] = frag(chunk_a(ca, jn, t));
+      for (int t = 0; t < C::RT; ++t) fa[t] = na[t];
 #pragma unroll
-        for (int t = 0; t < C::RT; ++t)
+      for (int t = 0; t < C::TT; ++t) fb[t] = nb[t];
+    };
+    int s = s0, after_a, after_b;
+    auto three_steps = [&] {
+      after_a = slot_a + C::kSlabA == C::SA * C::kSlabA ? 0 : slot_a + C::kSlabA;
+      after_b = slot_b + C::kSlabB == C::SB * C::kSlabB ? 0 : slot_b + C::kSlabB;
 #pragma unroll
-          for (int tt = 0; tt < C::TT; ++tt) acc[t][tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[t], fb[tt], acc[t][tt], 0, 0, 0);
-#pragma unroll
-        for (int t = 0; t < C::RT; ++t) fa[t] = na[t];
-#pragma unroll
-        for (int t = 0; t < C::TT; ++t) fb[t] = nb[t];
+      for (int j = 0; j < 3; ++j) {
+        step(slot_a, slot_b, j + 1, [](int) {});
 #pragma unroll
         for (int i = 0; i < C::RT + C::TT; ++i) {
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
@@ -158,6 +156,40 @@ struct HeadLoop {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+    };
+    const int limit = s1 < full ? s1 : full;
+    for (; next_a < limit && next_b < limit; ++s) {       // whole slabs to fetch: their requests go out between the matrix instructions
+      three_steps();
+      lds_wait_barrier<C::kAhead>();
+      const uint32_t dst_b = lds0 + (uint32_t)((C::SA * C::kSlabA + put_b + wave * 64) * 16), dst_a = lds0 + (uint32_t)((put_a + wave * 64) * 16);
+      const uint8_t* from_b = base_b + (int64_t)next_b * 128;
+      const uint8_t* from_a = base_a + (int64_t)next_a * 128;
+      step(after_a, after_b, 0, [&](int i) {
+        constexpr int kAll = C::IA + C::IB, kSteps = C::RT * C::TT;
+#pragma unroll
+        for (int r = i * kAll / kSteps; r < (i + 1) * kAll / kSteps; ++r) {
+          if (r < C::IB) lds_request(dst_b + (uint32_t)(r * C::kThreads * 16), from_b, off_b[r < C::IB ? r : 0]);
+          else lds_request(dst_a + (uint32_t)((r - C::IB) * C::kThreads * 16), from_a, off_a[r < C::IB ? 0 : r - C::IB]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      ++next_a;
+      ++next_b;
+      put_a = put_a + C::kSlabA == C::SA * C::kSlabA ? 0 : put_a + C::kSlabA;
+      put_b = put_b + C::kSlabB == C::SB * C::kSlabB ? 0 : put_b + C::kSlabB;
+      slot_a = after_a;
+      slot_b = after_b;
+    }
+    for (; s < s1; ++s) {
+      three_steps();
+      if (s + 1 < s1) {
+        meet(s + 1);
+        fetch_b();
+        fetch_a();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      step(after_a, after_b, 0, [](int) {});     // (behind the last stage the fragments are whatever the slots hold, and not used)
+      __builtin_amdgcn_sched_barrier(0);
       slot_a = after_a;
       slot_b = after_b;
     }
