@@ -590,12 +590,12 @@ QERL_API int lm_head_logprob_backward(const float* grad_logprob_f32, const float
  *   step can be replayed with another rate and step count.  If *grad_scale is not finite the step changes nothing.
  * lora_adamw_grad_norm: *norm = sqrt(sum g^2) over all gradients, summed in fp64 in a fixed order, and
  *   *scale = min(1, max_norm / (norm + 1e-6)), NaN if the norm is not finite: pass it as grad_scale.  norm may be NULL.
- *   workspace: lora_adamw_grad_norm_workspace_bytes() bytes, 256-byte aligned; needs no initialisation.
+ *   The sums of its workgroups pass through the table, so norms of one plan must be ordered on one stream, as its steps must.
  * lora_adamw_moments: the values of an 8-bit state as fp32, m and v [state elements] (inspection, checkpoints).
  * Errors: NULL pointers (copy_bf16 may be NULL); n < 0, n_tensors outside 1..2^20, more than 2^31 - 1 pieces of 2048
  * elements, memory that a step writes named twice, bits other than 8 and 32, step < 1, lr, weight_decay < 0 or not
  * finite, betas outside [0, 1), eps <= 0 (QERL_ERR_SHAPE); parameters, gradients, copies, m or v not 16-byte aligned
- * (QERL_ERR_ALIGN); table or workspace too small or misaligned (QERL_ERR_WORKSPACE).
+ * (QERL_ERR_ALIGN); table too small or misaligned (QERL_ERR_WORKSPACE).
  */
 typedef struct {
   float* param_f32;            /* [n] updated in place */
@@ -628,9 +628,7 @@ QERL_API int64_t lora_adamw_state_elements(const qerl_adamw_tensor* tensors, int
 QERL_API int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tensors, void* table, size_t table_bytes,
                                   qerl_adamw_plan* plan, void* stream);
 QERL_API int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_state* state, const qerl_adamw_hyper* hyper, void* stream);
-QERL_API size_t lora_adamw_grad_norm_workspace_bytes(void);                                         /* host */
-QERL_API int lora_adamw_grad_norm(const qerl_adamw_plan* plan, double max_norm, float* norm_f32, float* scale_f32,
-                                  void* workspace, size_t workspace_bytes, void* stream);
+QERL_API int lora_adamw_grad_norm(const qerl_adamw_plan* plan, double max_norm, float* norm_f32, float* scale_f32, void* stream);
 QERL_API int lora_adamw_moments(const qerl_adamw_plan* plan, const qerl_adamw_state* state, float* m_f32, float* v_f32, void* stream);
 
 /* ---------------------------------------------------------------------------

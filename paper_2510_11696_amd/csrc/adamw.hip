@@ -93,8 +93,9 @@ __device__ __forceinline__ uint32_t encode_v(float x, uint32_t field, uint32_t r
   return field == 255u || !(x > 0.f) ? 0u : c > 1u ? c : 1u;
 }
 
-__global__ __launch_bounds__(64) void adamw_table_kernel(const TableBatch batch, int count, AdamTensor* out) {
+__global__ __launch_bounds__(64) void adamw_table_kernel(const TableBatch batch, int count, AdamTensor* out, uint32_t* arrived) {
   const int i = threadIdx.x;
+  if (i == 0) *arrived = 0u;
   if (i < count) out[i] = batch.t[i];
 }
 __global__ __launch_bounds__(256) void adamw_owner_kernel(const AdamTensor* table, uint32_t* owner) {
@@ -221,9 +222,11 @@ __global__ __launch_bounds__(256) void adamw_moments_kernel(const uint8_t* mc, c
   }
 }
 
-// Sum of squares of all gradients: a workgroup sums a contiguous range of chunks in fp64 (a square of an fp32 value is exact there),
-// one more adds the workgroups' sums in a fixed order.
+// Sum of squares of all gradients: a workgroup sums a contiguous range of chunks in fp64 (a square of an fp32 value is exact there); the
+// last one to finish adds the workgroups' sums in their order, so that nothing depends on which one it was, and sets the counter back.
+// Sums and counter pass between the XCDs' caches by accesses at device scope.
 constexpr int kNormGroups = 1024;
+struct NormArea { double partial[kNormGroups]; uint32_t arrived; };
 __device__ __forceinline__ double block_sum64(double v, double* smem) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -231,8 +234,10 @@ __device__ __forceinline__ double block_sum64(double v, double* smem) {
   __syncthreads();
   return (smem[0] + smem[1]) + (smem[2] + smem[3]);
 }
-__global__ __launch_bounds__(256) void adamw_norm_kernel(const AdamTensor* table, const uint32_t* owner, int64_t chunks, double* partial) {
-  __shared__ double smem[4];
+__global__ __launch_bounds__(256) void adamw_norm_kernel(const AdamTensor* table, const uint32_t* owner, int64_t chunks, NormArea* area, double max_norm,
+                                                         float* norm, float* scale) {
+  __shared__ double smem[2][4];
+  __shared__ uint32_t order;
   const int64_t c0 = chunks * blockIdx.x / gridDim.x, c1 = chunks * (blockIdx.x + 1) / gridDim.x;
   double sum = 0.0;
   for (int64_t c = c0; c < c1; ++c) {
@@ -249,18 +254,24 @@ __global__ __launch_bounds__(256) void adamw_norm_kernel(const AdamTensor* table
       for (int64_t i = i0; i < t.n; ++i) sum += (double)t.g[i] * (double)t.g[i];
     }
   }
-  sum = block_sum64(sum, smem);
-  if (threadIdx.x == 0) partial[blockIdx.x] = sum;
-}
-__global__ __launch_bounds__(256) void adamw_norm_finish_kernel(const double* partial, int n, double max_norm, float* norm, float* scale) {
-  __shared__ double smem[4];
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < n; i += 256) sum += partial[i];
-  sum = block_sum64(sum, smem);
+  sum = block_sum64(sum, smem[0]);
+  uint64_t* partial = reinterpret_cast<uint64_t*>(area->partial);
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(partial + blockIdx.x, __builtin_bit_cast(uint64_t, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    order = __hip_atomic_fetch_add(&area->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (order != gridDim.x - 1) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  sum = 0.0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += 256)
+    sum += __builtin_bit_cast(double, __hip_atomic_load(partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+  sum = block_sum64(sum, smem[1]);
   if (threadIdx.x == 0) {
     const double r = sqrt(sum), s = max_norm / (r + 1e-6);
     if (norm) *norm = (float)r;
     *scale = isfinite(r) ? (float)(s < 1.0 ? s : 1.0) : __uint_as_float(0x7fc00000u);
+    __hip_atomic_store(&area->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
@@ -292,7 +303,10 @@ static int overlaps(const qerl_adamw_tensor* t, int n) {
   return bad;
 }
 
-struct AdamLayout { int64_t elements, chunks; size_t table_bytes, bytes; };
+// The table: what the norm's workgroups hand over, the tensors, the tensor of each chunk
+constexpr size_t kNormBytes = (sizeof(NormArea) + 255) & ~(size_t)255;
+static size_t owner_offset(int n) { return kNormBytes + (((size_t)n * sizeof(AdamTensor) + 255) & ~(size_t)255); }
+struct AdamLayout { int64_t elements, chunks; size_t bytes; };
 static bool adam_layout(const qerl_adamw_tensor* t, int n, AdamLayout& l) {
   if (!t || n < 1 || n > (1 << 20)) return false;
   l.elements = l.chunks = 0;
@@ -302,12 +316,12 @@ static bool adam_layout(const qerl_adamw_tensor* t, int n, AdamLayout& l) {
     l.chunks += ceil_div(t[i].n, kChunk);
     if (l.chunks > 0x7fffffff) return false;
   }
-  l.table_bytes = ((size_t)n * sizeof(AdamTensor) + 255) & ~(size_t)255;
-  l.bytes = (l.table_bytes + (size_t)l.chunks * 4 + 255) & ~(size_t)255;
+  l.bytes = (owner_offset(n) + (size_t)l.chunks * 4 + 255) & ~(size_t)255;
   return true;
 }
+static const AdamTensor* tensors_of(const qerl_adamw_plan* p) { return reinterpret_cast<const AdamTensor*>(static_cast<const uint8_t*>(p->table) + kNormBytes); }
 static const uint32_t* owner_of(const qerl_adamw_plan* p) {
-  return reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p->table) + (((size_t)p->n_tensors * sizeof(AdamTensor) + 255) & ~(size_t)255));
+  return reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p->table) + owner_offset(p->n_tensors));
 }
 static int plan_status(const qerl_adamw_plan* p) {
   if (!p) return QERL_ERR_NULL;
@@ -342,7 +356,7 @@ extern "C" int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tens
   if (const int o = overlaps(tensors, n_tensors)) return o > 0 ? QERL_ERR_SHAPE : QERL_ERR_WORKSPACE;
   if (!table || table_bytes < l.bytes) return QERL_ERR_WORKSPACE;
   if (!aligned(table, 256)) return QERL_ERR_WORKSPACE;
-  AdamTensor* out = static_cast<AdamTensor*>(table);
+  AdamTensor* out = reinterpret_cast<AdamTensor*>(static_cast<uint8_t*>(table) + kNormBytes);
   TableBatch batch = {};
   int64_t state0 = 0, chunk0 = 0;
   for (int i = 0; i < n_tensors; ++i) {
@@ -351,7 +365,7 @@ extern "C" int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tens
     state0 += ceil_div(t.n, kStateBlock) * kStateBlock;
     chunk0 += ceil_div(t.n, kChunk);
     if (i % kTableBatch == kTableBatch - 1 || i == n_tensors - 1)
-      adamw_table_kernel<<<dim3(1), dim3(64), 0, (hipStream_t)stream>>>(batch, i % kTableBatch + 1, out + i / kTableBatch * kTableBatch);
+      adamw_table_kernel<<<dim3(1), dim3(64), 0, (hipStream_t)stream>>>(batch, i % kTableBatch + 1, out + i / kTableBatch * kTableBatch, &static_cast<NormArea*>(table)->arrived);
   }
   *plan = qerl_adamw_plan{table, l.elements, l.chunks, n_tensors};
   if (l.chunks > 0)
@@ -377,7 +391,7 @@ extern "C" int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_sta
   if (!aligned(h->lr_device, 4) || !aligned(h->step_device, 8) || !aligned(h->grad_scale, 4)) return QERL_ERR_ALIGN;
   if (plan->chunks == 0) return QERL_OK;
   AdamArgs a = {};
-  a.table = static_cast<const AdamTensor*>(plan->table);
+  a.table = tensors_of(plan);
   a.owner = owner_of(plan);
   a.m = state->m; a.v = state->v; a.ms = state->m_scale; a.vs = state->v_scale;
   a.b1 = (float)h->beta1; a.omb1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.omb2 = (float)(1.0 - h->beta2); a.eps = (float)h->eps;
@@ -414,18 +428,13 @@ extern "C" int lora_adamw_moments(const qerl_adamw_plan* plan, const qerl_adamw_
   return launch_status();
 }
 
-extern "C" size_t lora_adamw_grad_norm_workspace_bytes(void) { return kNormGroups * sizeof(double); }
-extern "C" int lora_adamw_grad_norm(const qerl_adamw_plan* plan, double max_norm, float* norm, float* scale, void* workspace,
-                                    size_t workspace_bytes, void* stream) {
+extern "C" int lora_adamw_grad_norm(const qerl_adamw_plan* plan, double max_norm, float* norm, float* scale, void* stream) {
   if (const int e = plan_status(plan)) return e;
   if (!scale) return QERL_ERR_NULL;
   if (!(max_norm > 0)) return QERL_ERR_SHAPE;
   if (!aligned(scale, 4) || !aligned(norm, 4)) return QERL_ERR_ALIGN;
-  if (!workspace || workspace_bytes < kNormGroups * sizeof(double) || !aligned(workspace, 256)) return QERL_ERR_WORKSPACE;
-  double* partial = static_cast<double*>(workspace);
-  const int n = (int)(plan->chunks < kNormGroups ? plan->chunks : kNormGroups);
-  if (n > 0)
-    adamw_norm_kernel<<<dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream>>>(static_cast<const AdamTensor*>(plan->table), owner_of(plan), plan->chunks, partial);
-  adamw_norm_finish_kernel<<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(partial, n, max_norm, norm, scale);
+  const int n = plan->chunks < 1 ? 1 : (int)(plan->chunks < kNormGroups ? plan->chunks : kNormGroups);
+  adamw_norm_kernel<<<dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream>>>(tensors_of(plan), owner_of(plan), plan->chunks, static_cast<NormArea*>(const_cast<void*>(plan->table)),
+                                                                           max_norm, norm, scale);
   return launch_status();
 }

@@ -150,13 +150,12 @@ def test_moments_in_8_bits_follow_a_steady_gradient():
 def test_captured_step_with_rate_and_count_on_the_device(bits):
     a, b = _Set([3001, 64], bits, 20), _Set([3001, 64], bits, 20)
     lr, step = torch.tensor([0.0], device="cuda"), torch.tensor([0], device="cuda")
-    ws = torch.empty((1 << 14,), dtype=torch.uint8, device="cuda")
     out = (torch.empty((1,), device="cuda"), torch.empty((1,), device="cuda"))
     h = {k: v for k, v in HYPER.items() if k != "lr"}
 
     def work():
         step.add_(1)
-        qerl.lora_adamw_grad_norm(a.plan, 0.3, workspace=ws, out=out)
+        qerl.lora_adamw_grad_norm(a.plan, 0.3, out=out)
         qerl.lora_adamw_step(a.plan, lr_device=lr, step_device=step, seed=5, grad_scale=out[1], **h)
     graph = torch.cuda.CUDAGraph()
     a.gradients()
