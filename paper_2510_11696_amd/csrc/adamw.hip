@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256) void adamw_moments_kernel(const uint8_t* mc, c
 // Sum of squares of all gradients: a workgroup sums a contiguous range of chunks in fp64 (a square of an fp32 value is exact there); the
 // last one to finish adds the workgroups' sums in their order, so that nothing depends on which one it was, and sets the counter back.
 // Sums and counter pass between the XCDs' caches by accesses at device scope.
-constexpr int kNormGroups = 1024;
+constexpr int kNormGroups = 2048, kNormAhead = 4;
 struct NormArea { double partial[kNormGroups]; uint32_t arrived; };
 __device__ __forceinline__ double block_sum64(double v, double* smem) {
 #pragma unroll
@@ -240,29 +240,41 @@ __global__ __launch_bounds__(256) void adamw_norm_kernel(const AdamTensor* table
   __shared__ uint32_t order;
   const int64_t c0 = chunks * blockIdx.x / gridDim.x, c1 = chunks * (blockIdx.x + 1) / gridDim.x;
   double sum = 0.0;
-  for (int64_t c = c0; c < c1; ++c) {
-    const AdamTensor t = table[owner[c]];
-    const int64_t i0 = (c - t.chunk0) * kChunk + (int64_t)threadIdx.x * 8;
-    if (i0 + 8 <= t.n) {
+  for (int64_t c = c0; c < c1; c += kNormAhead) {       // some chunks at a time: their places, then their values, are all on their way together
+    const float* g[kNormAhead];
+    int left[kNormAhead];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 g = *reinterpret_cast<const f32x4*>(t.g + i0 + 4 * h);
+    for (int u = 0; u < kNormAhead; ++u) {
+      const int64_t at = c + u < c1 ? c + u : c1 - 1;
+      const AdamTensor t = table[owner[at]];
+      const int64_t i0 = (at - t.chunk0) * kChunk + (int64_t)threadIdx.x * 8, rest = c + u < c1 ? t.n - i0 : 0;
+      g[u] = t.g + i0;
+      left[u] = rest >= 8 ? 8 : rest > 0 ? (int)rest : 0;
+    }
+    f32x4 v[kNormAhead][2] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum += (double)g[j] * (double)g[j];
+    for (int u = 0; u < kNormAhead; ++u)
+      if (left[u] == 8) {
+        v[u][0] = *reinterpret_cast<const f32x4*>(g[u]);
+        v[u][1] = *reinterpret_cast<const f32x4*>(g[u] + 4);
       }
-    } else {
-      for (int64_t i = i0; i < t.n; ++i) sum += (double)t.g[i] * (double)t.g[i];
+#pragma unroll
+    for (int u = 0; u < kNormAhead; ++u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += (double)v[u][j >> 2][j & 3] * (double)v[u][j >> 2][j & 3];
+      if (left[u] < 8)
+        for (int j = 0; j < left[u]; ++j) sum += (double)g[u][j] * (double)g[u][j];
     }
   }
   sum = block_sum64(sum, smem[0]);
   uint64_t* partial = reinterpret_cast<uint64_t*>(area->partial);
   if (threadIdx.x == 0) {
     __hip_atomic_store(partial + blockIdx.x, __builtin_bit_cast(uint64_t, sum), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    order = __hip_atomic_fetch_add(&area->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the sum is where all see it before the count is; a release would write the L2 back
+    order = __hip_atomic_fetch_add(&area->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   if (order != gridDim.x - 1) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   sum = 0.0;
   for (int i = threadIdx.x; i < (int)gridDim.x; i += 256)
     sum += __builtin_bit_cast(double, __hip_atomic_load(partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
