@@ -173,15 +173,30 @@ __global__ __launch_bounds__(256) void head_backward_kernel(const float* g, cons
       u32x4{pack_bf16x2(gm * a[0], gm * a[1]), pack_bf16x2(gm * a[2], gm * a[3]), pack_bf16x2(gm * b[0], gm * b[1]), pack_bf16x2(gm * b[2], gm * b[3])};
 }
 
-// W [V, ldw] -> Wt [H, ldt], ldt = V rounded up to 64, zeros behind the vocabulary
+// W [V, ldw] -> Wt [H, ldt], ldt = V rounded up to 64, zeros behind the vocabulary.  Tiles of 64 x 64, 16 bytes a lane on both sides; the
+// swizzle of the 16-byte columns keeps the column reads off each other's banks.
 __global__ __launch_bounds__(256) void head_transpose_kernel(const uint16_t* w, int64_t V, int64_t H, int64_t ldw, uint16_t* out, int64_t ldt) {
-  __shared__ uint16_t tile[64][66];
+  __shared__ __attribute__((aligned(16))) uint16_t tile[64 * 64];
   const int64_t v0 = (int64_t)blockIdx.x * 64, h0 = (int64_t)blockIdx.y * 64;
-  const int c = threadIdx.x & 63;
-  for (int r = threadIdx.x >> 6; r < 64; r += 4) tile[r][c] = v0 + r < V && h0 + c < H ? w[(v0 + r) * ldw + h0 + c] : 0;
+  const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    const int row = r + i;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (v0 + row < V && h0 + 8 * c < H) v = *reinterpret_cast<const u32x4*>(w + (v0 + row) * ldw + h0 + 8 * c);   // H is a multiple of 8
+    *reinterpret_cast<u32x4*>(tile + row * 64 + 8 * (c ^ (row >> 3))) = v;
+  }
   __syncthreads();
-  for (int r = threadIdx.x >> 6; r < 64; r += 4)
-    if (h0 + r < H) out[(h0 + r) * ldt + v0 + c] = tile[c][r];
+#pragma unroll
+  for (int i = 0; i < 64; i += 32) {
+    const int h = r + i;                          // a row of the output, its vocabulary rows 8 c .. 8 c + 7
+    if (h0 + h >= H) continue;
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      o[j] = tile[(8 * c + 2 * j) * 64 + 8 * ((h >> 3) ^ c) + (h & 7)] | (uint32_t)tile[(8 * c + 2 * j + 1) * 64 + 8 * ((h >> 3) ^ c) + (h & 7)] << 16;
+    *reinterpret_cast<u32x4*>(out + (h0 + h) * ldt + v0 + 8 * c) = u32x4{o[0], o[1], o[2], o[3]};
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
@@ -212,7 +227,7 @@ static int64_t piece_blocks(int64_t blocks, int64_t most, int64_t token_blocks) 
 static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
   HeadPlan q = {};
   q.tokens = M < kTokenBlock ? M : kTokenBlock;
-  q.gemm = plan_head_gemm(q.tokens, gradient);
+  q.gemm = plan_head_gemm(q.tokens, V, gradient);
   q.compact = q.tokens > 128;                             // fewer are one token block whatever they are
   q.parts = ceil_div(V, q.gemm.part_rows);
   auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };

@@ -35,7 +35,7 @@ __device__ __forceinline__ int head_row(const HeadArgs& a, int token) { return a
 
 // the matrix kernels (lm_head_gemm.hip)
 struct HeadGemmPlan { int tokens, rows, part_rows; };   // tokens and vocabulary rows of a tile, rows of a part
-HeadGemmPlan plan_head_gemm(int64_t M, bool gradient);
+HeadGemmPlan plan_head_gemm(int64_t M, int64_t V, bool gradient);
 int launch_head_logits(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
 int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
 // the sums: rows of a tile, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them

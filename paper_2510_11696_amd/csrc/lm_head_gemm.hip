@@ -383,14 +383,14 @@ __host__ __device__ inline int head_units_per_xcd(int log_split, int row_blocks,
   return ((row_blocks + (1 << h.rows) - 1) >> h.rows) * ((token_blocks + (1 << h.tokens) - 1) >> h.tokens);
 }
 
-// log2 of how many parts K is split into: rounds of units over the chip's compute units (two at a time for the smallest tile) at 1.6 us a
-// stage of 256 x 256 or what the row slab takes from memory (32 KB per unit at 6 TB/s over the chip: 1.4 us), 2 us to start a unit, and the
+// log2 of how many parts K is split into: rounds of units over the chip's compute units (two at a time for the smallest tile) at 0.4 us a
+// stage and 1.2 per 256 x 256 of it, or what the row slab takes from memory (32 KB per unit at 6 TB/s over the chip: 1.4 us), 2 us to start a unit, and the
 // partial sums at 5 TB/s, which every piece reads and writes.  Whole nanoseconds: the host sizes the sums by the same function that the
 // kernels evaluate for the rows that have a loss.
 struct HeadSplit { int log_split; int64_t ns; };
 template <int ROWS, int TOKENS>
 __host__ __device__ inline HeadSplit head_split(int row_blocks, int token_blocks, int stages) {
-  constexpr int kAtOnce = TOKENS == 64 ? 64 : 32, kStage = TOKENS == 256 ? 1600 * ROWS / 256 : 1400 * ROWS / 256 * kAtOnce / 32,
+  constexpr int kAtOnce = TOKENS == 64 ? 64 : 32, kStage = TOKENS == 256 ? 400 + 1200 * ROWS / 256 : 1400 * ROWS / 256 * kAtOnce / 32,
                 kTile = 2 * ROWS * TOKENS * 4 / 5000;
   HeadSplit best = {0, INT64_MAX};
   for (int l = 0; l <= 6 && (l == 0 || 1 << l <= stages); ++l) {
@@ -508,13 +508,16 @@ using Head32 = HeadCfg<2, 1, 2, 1, 4, 4>;        // 128 rows x 32 tokens, two wo
 using Head64 = HeadCfg<2, 2, 2, 1, 3, 3>;        // 128 rows x 64 tokens
 using Head128 = HeadCfg<2, 2, 4, 2, 3, 2>;       // 256 rows x 128 tokens
 using Head256 = HeadCfg<4, 2, 2, 4, 3, 2>;       // 256 rows x 256 tokens
+using HeadHalf = HeadCfg<2, 2, 2, 4, 3, 2>;      // 128 rows x 256 tokens
 using Head320 = HeadCfg<5, 2, 2, 4, 2, 2>;       // 320 rows x 256 tokens: sums whose tiles of 256 would leave a round of workgroups half empty
 
-// The smallest tile that holds all tokens, so that few tokens stream the weights through small workgroups
-HeadGemmPlan plan_head_gemm(int64_t M, bool gradient) {
+// The smallest tile that holds all tokens, so that few tokens stream the weights through small workgroups; beyond 128 tokens 256 rows, or 128
+// where those would leave half of the compute units without a tile (200 rows of 32001 x 1024: 35 -> 25 us).
+HeadGemmPlan plan_head_gemm(int64_t M, int64_t V, bool gradient) {
   if (M <= 32 && !gradient) return HeadGemmPlan{Head32::kTokens, Head32::kRows, 32 * Head32::RT};
   if (M <= 64) return HeadGemmPlan{Head64::kTokens, Head64::kRows, 32 * Head64::RT};
   if (M <= 128) return HeadGemmPlan{Head128::kTokens, Head128::kRows, 32 * Head128::RT};
+  if (ceil_div(V, Head256::kRows) * ceil_div(M, Head256::kTokens) <= 128) return HeadGemmPlan{HeadHalf::kTokens, HeadHalf::kRows, 32 * HeadHalf::RT};
   return HeadGemmPlan{Head256::kTokens, Head256::kRows, 32 * Head256::RT};
 }
 
@@ -557,14 +560,14 @@ int launch_head_logits(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, h
     case 32: return launch_mode<Head32, false>(entropy, a, st);
     case 64: return launch_mode<Head64, false>(entropy, a, st);
     case 128: return launch_mode<Head128, false>(entropy, a, st);
-    default: return launch_mode<Head256, false>(entropy, a, st);
+    default: return p.rows == 128 ? launch_mode<HeadHalf, false>(entropy, a, st) : launch_mode<Head256, false>(entropy, a, st);
   }
 }
 int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st) {
   switch (p.tokens) {
     case 64: return launch_mode<Head64, true>(entropy, a, st);
     case 128: return launch_mode<Head128, true>(entropy, a, st);
-    default: return launch_mode<Head256, true>(entropy, a, st);
+    default: return p.rows == 128 ? launch_mode<HeadHalf, true>(entropy, a, st) : launch_mode<Head256, true>(entropy, a, st);
   }
 }
 
@@ -587,6 +590,7 @@ HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t
   if (p.tokens == 64) consider_sums<Head64>(q, best, M, H, piece);
   else if (p.tokens == 128) consider_sums<Head128>(q, best, M, H, piece);
   else {
+    consider_sums<HeadHalf>(q, best, M, H, piece);
     consider_sums<Head256>(q, best, M, H, piece);
     consider_sums<Head320>(q, best, M, H, piece);
   }
@@ -604,6 +608,7 @@ static int launch_slope(const HeadArgs& sums, const HeadArgs& head, float inv_te
 int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st) {
   return p.tokens == 64    ? launch_sums<Head64>(a, st)
          : p.tokens == 128 ? launch_sums<Head128>(a, st)
+         : q.rows == 128   ? launch_sums<HeadHalf>(a, st)
          : q.rows == 320   ? launch_sums<Head320>(a, st)
                            : launch_sums<Head256>(a, st);
 }
@@ -611,6 +616,7 @@ int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadAr
                       const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st) {
   return p.tokens == 64    ? launch_slope<Head64>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
          : p.tokens == 128 ? launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
+         : q.rows == 128   ? launch_slope<HeadHalf>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
          : q.rows == 320   ? launch_slope<Head320>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
                            : launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
 }
