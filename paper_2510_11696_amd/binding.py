@@ -495,6 +495,8 @@ def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_sca
     Bs = Bs if Bs is not None else [None] * n
     lora_scales = lora_scales if lora_scales is not None else [0.0] * n
     M, K, ldx = _rows(x, "x")
+    if any(v is not None and len(v) != n for v in (dAs, dBs)):
+        raise ValueError("dAs and dBs must have a place for every member")
     descs = (_BackwardDesc * n)()
     grads, keep = [], []
     for i, (dy, w) in enumerate(zip(dys, weights)):
@@ -514,6 +516,8 @@ def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_sca
             dB = _grad_buffer(dBs[i] if dBs is not None else None, (N, r), x.device, "dB")
             d.A, d.B, d.r, d.lora_scale = _dev(A, torch.bfloat16, "A"), _dev(B, torch.bfloat16, "B"), r, float(lora_scales[i])
             d.dA, d.dB = _dev(dA, torch.float32, "dA"), _dev(dB, torch.float32, "dB")
+        elif any(v is not None and v[i] is not None for v in (dAs, dBs)):
+            raise ValueError("dA and dB belong to an adapter")
         grads.append((dA, dB))
         keep.append((dy, A, B))
     dx = torch.empty((M, K), dtype=torch.bfloat16, device=x.device)

@@ -115,7 +115,9 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   int64_t step = a.step;
   if constexpr (DEVICE_HYPER) {
     if (a.step_dev) step = *a.step_dev;
-    const AdamFactors f = adam_factors(a.lr_dev ? (double)*a.lr_dev : a.lr, a.beta1, a.beta2, a.wd, step);
+    const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
+    if (step < 1 || !(lr >= 0.0) || !isfinite(lr)) return;   // what the host refuses
+    const AdamFactors f = adam_factors(lr, a.beta1, a.beta2, a.wd, step);
     decay = f.decay; step_size = f.step_size; isb2 = f.isb2;
   }
   const uint32_t chunk = blockIdx.x;
@@ -385,16 +387,27 @@ extern "C" int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tens
   return launch_status();
 }
 
-static int state_status(const qerl_adamw_state* s) {
+static bool apart(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x + na <= y || y + nb <= x;
+}
+static int state_status(const qerl_adamw_state* s, int64_t elements) {
   if (!s) return QERL_ERR_NULL;
   if (s->bits != 8 && s->bits != 32) return QERL_ERR_SHAPE;
+  if (elements == 0) return QERL_OK;
   if (!s->m || !s->v || (s->bits == 8 && (!s->m_scale || !s->v_scale))) return QERL_ERR_NULL;
-  return aligned(s->m, 16) && aligned(s->v, 16) ? QERL_OK : QERL_ERR_ALIGN;
+  if (!aligned(s->m, 16) || !aligned(s->v, 16)) return QERL_ERR_ALIGN;
+  const size_t n = (size_t)elements * (s->bits / 8), b = (size_t)elements / kStateBlock;
+  if (!apart(s->m, n, s->v, n)) return QERL_ERR_SHAPE;
+  if (s->bits == 8 && !(apart(s->m_scale, b, s->v_scale, b) && apart(s->m, n, s->m_scale, b) && apart(s->m, n, s->v_scale, b) &&
+                        apart(s->v, n, s->m_scale, b) && apart(s->v, n, s->v_scale, b)))
+    return QERL_ERR_SHAPE;
+  return QERL_OK;
 }
 
 extern "C" int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_state* state, const qerl_adamw_hyper* h, void* stream) {
   if (const int e = plan_status(plan)) return e;
-  if (const int e = state_status(state)) return e;
+  if (const int e = state_status(state, plan->elements)) return e;
   if (!h) return QERL_ERR_NULL;
   const bool lr_ok = h->lr_device || (isfinite(h->lr) && h->lr >= 0), step_ok = h->step_device || h->step >= 1;
   if (!lr_ok || !step_ok || !(h->beta1 >= 0 && h->beta1 < 1) || !(h->beta2 >= 0 && h->beta2 < 1) || !(h->eps > 0 && isfinite(h->eps)) ||
@@ -429,12 +442,12 @@ extern "C" int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_sta
 
 extern "C" int lora_adamw_moments(const qerl_adamw_plan* plan, const qerl_adamw_state* state, float* m, float* v, void* stream) {
   if (const int e = plan_status(plan)) return e;
-  if (const int e = state_status(state)) return e;
+  if (const int e = state_status(state, plan->elements)) return e;
   if (state->bits != 8) return QERL_ERR_SHAPE;
-  if (!m || !v) return QERL_ERR_NULL;
-  if (!aligned(m, 16) || !aligned(v, 16)) return QERL_ERR_ALIGN;
   const int64_t groups = plan->elements / 8;
   if (groups == 0) return QERL_OK;
+  if (!m || !v) return QERL_ERR_NULL;
+  if (!aligned(m, 16) || !aligned(v, 16)) return QERL_ERR_ALIGN;
   adamw_moments_kernel<<<dim3((unsigned)ceil_div(groups, 256)), dim3(256), 0, (hipStream_t)stream>>>(
       static_cast<const uint8_t*>(state->m), static_cast<const uint8_t*>(state->v), state->m_scale, state->v_scale, groups, m, v);
   return launch_status();

@@ -312,7 +312,7 @@ static int run_head(const HeadCall& c, bool gradient) {
   if (c.M < 0 || c.V < 1 || c.V > kMaxVocab || c.H < 8 || c.H % 8 != 0 || c.M > 0x7fffffff || c.ldx < c.H || c.ldx >= kMaxLd || c.ldw < c.H ||
       c.ldw >= kMaxLd || (gradient && c.ld_slope < c.H))
     return QERL_ERR_SHAPE;
-  if (!(c.inv_temperature > 0.f) || !isfinite(c.inv_temperature)) return QERL_ERR_SHAPE;
+  if (!(c.inv_temperature > 0.f) || !isfinite(c.inv_temperature * 1.44269504088896341f)) return QERL_ERR_SHAPE;
   if (c.M == 0) return QERL_OK;
   if (!c.x || !c.W || !c.targets || !c.logprob || (gradient && (!c.Wt || !c.slope))) return QERL_ERR_NULL;
   if (!aligned(c.x, 16) || !aligned(c.W, 16) || !aligned(c.Wt, 16) || !aligned(c.slope, 16) || c.ldx % 8 || c.ldw % 8 || (gradient && c.ld_slope % 4) ||

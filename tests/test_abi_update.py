@@ -38,7 +38,7 @@ def test_logprob_refusals(lib, gradient):
     call = lambda **kw: _logprob(lib, gradient, **kw)
     assert call(M=0) == 0 and call(M=0, x=None, W=None) == 0
     for kw in (dict(M=-1), dict(V=0), dict(H=0), dict(H=60, ldx=64), dict(H=4), dict(ldx=56), dict(ldw=56), dict(V=(1 << 22) + 1), dict(M=1 << 31), dict(ldx=1 << 18), dict(ldw=1 << 18),
-               dict(it=0.0), dict(it=-1.0), dict(it=float("inf")), dict(it=float("nan"))):
+               dict(it=0.0), dict(it=-1.0), dict(it=float("inf")), dict(it=float("nan")), dict(it=3e38)):
         assert call(**kw) == SHAPE, kw
     for k in ("x", "W", "targets", "lp"):
         assert call(**{k: None}) == NULL, k
@@ -115,7 +115,7 @@ def test_adamw_plan_refusals(lib):
 def test_adamw_step_norm_and_moments_refusals(lib):
     def step(plan=None, state=None, **kw):
         pl = _AdamWPlanStruct(FAKE, 1024, 1, 1)
-        st = _AdamWState(8, FAKE, FAKE, FAKE, FAKE)
+        st = _AdamWState(8, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE)
         for d, src in ((pl, plan), (st, state)):
             for k, v in (src or {}).items():
                 setattr(d, k, v)
@@ -129,8 +129,12 @@ def test_adamw_step_norm_and_moments_refusals(lib):
         assert step(**kw) == SHAPE, kw
     assert step(lr=nan, lr_device=FAKE + 2) == ALIGN and step(step=0, step_device=FAKE + 4) == ALIGN and step(grad_scale=FAKE + 1) == ALIGN
     assert step(state=dict(bits=16)) == SHAPE and step(state=dict(m=None)) == NULL and step(state=dict(v_scale=None)) == NULL
-    assert step(state=dict(m=FAKE + 8)) == ALIGN and step(plan=dict(table=None)) == NULL and step(plan=dict(chunks=-1)) == SHAPE
-    pl, st = _AdamWPlanStruct(FAKE, 1024, 1, 1), _AdamWState(8, FAKE, FAKE, FAKE, FAKE)
+    for kw in (dict(v=2 * FAKE), dict(v=2 * FAKE + 1008), dict(m_scale=2 * FAKE), dict(v_scale=3 * FAKE + 16), dict(v_scale=4 * FAKE + 31),
+               dict(bits=32, v=2 * FAKE + 4080)):                                # parts of the state that share memory
+        assert step(state=kw) == SHAPE, kw
+    assert step(plan=dict(elements=0, chunks=0), state=dict(m=None, v=None)) == 0
+    assert step(state=dict(m=2 * FAKE + 8)) == ALIGN and step(plan=dict(table=None)) == NULL and step(plan=dict(chunks=-1)) == SHAPE
+    pl, st = _AdamWPlanStruct(FAKE, 1024, 1, 1), _AdamWState(8, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE)
     pb, sb = ctypes.byref(pl), ctypes.byref(st)
     assert lib.lora_adamw_step(None, sb, ctypes.byref(_AdamWHyper()), None) == NULL and lib.lora_adamw_step(pb, None, ctypes.byref(_AdamWHyper()), None) == NULL
     assert lib.lora_adamw_step(pb, sb, None, None) == NULL

@@ -190,6 +190,59 @@ def test_state_given_by_the_caller_and_its_gaps():
     assert not bool(m.cpu()[~inside].any()) and not bool(v.cpu()[~inside].any()) and bool((m.cpu()[inside] > 2).all())
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_captured_values_that_the_host_would_refuse_change_nothing(bits):
+    s = _Set([500], bits, 2, copies=False)
+    s.gradients()
+    lr, step = torch.tensor([1e-3], device="cuda"), torch.tensor([1], device="cuda")
+    h = {k: v for k, v in HYPER.items() if k != "lr"}
+    for bad_lr, bad_step in ((1e-3, 0), (1e-3, -5), (-1.0, 1), (float("nan"), 1), (float("inf"), 1)):
+        lr.fill_(bad_lr)
+        step.fill_(bad_step)
+        qerl.lora_adamw_step(s.plan, lr_device=lr, step_device=step, **h)
+        s.check()
+
+
+def test_nothing_to_do():
+    e = lambda: torch.empty((0,), device="cuda")
+    for bits in (8, 32):
+        plan = qerl.lora_adamw_plan([e(), e()], [e(), e()], state_bits=bits)
+        qerl.lora_adamw_step(plan, lr=1e-3, step=1)
+        norm, scale = qerl.lora_adamw_grad_norm(plan, 1.0)
+        assert norm.item() == 0 and scale.item() == 1
+    plan = qerl.lora_adamw_plan([e()], [e()])
+    assert qerl.lora_adamw_moments(plan)[0].numel() == 0
+
+
+def test_more_elements_than_32_bits_count():
+    """2^31 + 40 elements of one tensor and a few of another behind it, constant but for marked places."""
+    n = 2 ** 31 + 40
+    p, g = torch.zeros((n,), device="cuda"), torch.full((n,), 2.0 ** -10, device="cuda")
+    at = torch.tensor([0, 1, 2 ** 31 - 1, 2 ** 31, n - 1], device="cuda")
+    g[at] = torch.tensor([0.5, -0.25, 0.125, -1.0, 0.75], device="cuda")
+    p2, g2 = torch.ones((5,), device="cuda"), torch.full((5,), 0.5, device="cuda")
+    plan = qerl.lora_adamw_plan([p, p2], [g, g2], state_bits=8)
+    norm, scale = qerl.lora_adamw_grad_norm(plan, 1e9)
+    want = ((n - 5) * 2.0 ** -20 + sum(x * x for x in (0.5, 0.25, 0.125, 1.0, 0.75)) + 5 * 0.25) ** 0.5
+    assert abs(norm.item() - want) <= 2.0 ** -23 * want and scale.item() == 1
+    qerl.lora_adamw_step(plan, step=1, seed=3, **HYPER)
+    idx = torch.cat([at, torch.tensor([12345, 2 ** 31 + 7], device="cuda")])
+    ref, m, v = uo.adamw(np.zeros(7), g[idx].cpu().numpy(), np.zeros(7), np.zeros(7), step=1, **HYPER)
+    assert np.array_equal(p[idx].cpu().numpy(), ref)
+    ref2, _, _ = uo.adamw(np.ones(5), g2.cpu().numpy(), np.zeros(5), np.zeros(5), step=1, **HYPER)
+    assert np.array_equal(p2.cpu().numpy(), ref2)
+    # moments: within one rounding up of a step of 2^-3, and the first block against the oracle with its random bits
+    u = uo.random_fractions(32, 1, 3)
+    first = np.full(32, 2.0 ** -10, np.float32)
+    first[:2] = 0.5, -0.25
+    _, m, v = uo.adamw(np.zeros(32), first, np.zeros(32), np.zeros(32), step=1, **HYPER)
+    c, f = uo.encode_first(m, u)
+    assert np.array_equal(plan.m[:32].cpu().numpy(), c) and plan.m_scale[0].item() == f[0]
+    last = 2 ** 31 // 32                                                    # the block that begins at 2^31
+    assert plan.m_scale[last].item() == int(np.float32(np.float32(0.1) * np.float32(1.0)).view(np.uint32) >> 23)
+    assert bool((plan.m[n:2 ** 31 + 64] == 0).all())
+
+
 def test_binding_refusals():
     t = lambda n=8, dt=torch.float32: torch.zeros((n,), dtype=dt, device="cuda")
     for bad in (lambda: qerl.lora_adamw_plan([t()], [t(9)]), lambda: qerl.lora_adamw_plan([t(), t()], [t()]), lambda: qerl.lora_adamw_plan([t()], [t()], state_bits=16),

@@ -91,6 +91,81 @@ def test_logprob_and_slope(M, V, H, inv_t):
     assert torch.equal(qerl.lm_head_logprob(x, head, td, inv_t)[0], lp)
 
 
+def _check_on_gpu(x, head, t, inv_t, got, what, chunk=16384):
+    """The same bounds with the fp64 reference on the GPU, the vocabulary in chunks; got: (logprob, lse, entropy[, slope])."""
+    M, H = x.shape
+    V = head.V
+    xd, row = x.double(), torch.arange(M, device="cuda")
+    pieces = [slice(a, min(a + chunk, V)) for a in range(0, V, chunk)]
+    z = torch.cat([torch.matmul(xd, head.weight[c].double().t()) for c in pieces], 1) * inv_t
+    size = torch.stack([torch.matmul(xd.abs(), head.weight[c].double().abs().t()).amax(1) for c in pieces]).amax(0) * inv_t
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    ent = lse - (p * z).sum(1)
+    zt = z[row, t]
+    z[row, t] = -float("inf")
+    lp = -torch.log1p(torch.exp(z - zt[:, None]).sum(1))
+    z[row, t] = zt
+    D = 2 * ((H / 16 + 24) * U * size + 4 * U * z.abs().amax(1))
+    tol = [(D + 2.0 ** -17) * lp.abs().clamp(max=1) + 2.0 ** -22 * lp.abs(), D + 2.0 ** -17 + 2.0 ** -22 * lse.abs(),
+           (D + 2.0 ** -16) * (2 + (z - lse[:, None]).abs().amax(1))]
+    ref = [lp, lse, ent]
+    if len(got) == 4:
+        p[row, t] = 0
+        Wt = head.weight[t].double()
+        rest, D = p.sum(1, keepdim=True), D[:, None]
+        slope, mag = rest * Wt, torch.zeros((M, H), dtype=torch.float64, device="cuda")
+        for c in pieces:
+            w = head.weight[c].double()
+            slope -= torch.matmul(p[:, c], w)
+            mag += torch.matmul(p[:, c], w.abs())
+        ref.append(inv_t * slope)
+        tol.append(inv_t * ((D + 2.0 ** -16) * rest * Wt.abs() + (2.0 ** -8 + D + 2.0 ** -16 + (V / 16 + 64) * U) * mag))
+    for name, a, r, e in zip(("logprob", "lse", "entropy", "slope"), got, ref, tol):
+        off = (a.double() - r).abs() - e
+        assert bool(torch.isfinite(a).all()) and bool((off <= 0).all()), (what, name, float(off.max()))
+
+
+# sizes at which whole tiles fill the chip (256 rows x 256 rows of the vocabulary), with every kind of remainder; 4096 x 5120 takes the sums'
+# tiles of 320; 8192 rows take the vocabulary in pieces
+LARGE = [(257, 16640, 64), (300, 17001, 72), (511, 16577, 136), (700, 12007, 1000), (1025, 8193, 328), (2049, 4097, 192), (3000, 3001, 520), (4096, 1500, 5120),
+         (8192, 25000, 264)]
+
+
+@pytest.mark.parametrize("M,V,H", LARGE)
+def test_whole_tiles(M, V, H):
+    print("large case", M, V, H, flush=True)
+    x, W, t = _inputs(M, V, H, 300 + M)
+    head, td = qerl.lm_head_prepack(W), t.cuda()
+    wt = head.weight_t
+    assert torch.equal(wt[:, :V], W.t()) and not bool(wt[:, V:].any())
+    pick = torch.randperm(M, generator=torch.Generator().manual_seed(M))[:700].cuda()
+    for got in (qerl.lm_head_logprob(x, head, td, 0.8, entropy=True), qerl.lm_head_logprob_grad(x, head, td, 0.8, entropy=True)):
+        _check_on_gpu(x[pick], head, td[pick], 0.8, [a[pick] for a in got], (M, V, H))
+    # half of the rows without a loss: the others as they were, up to the order of sums
+    some = td.clone()
+    some[::2] = -1
+    part = qerl.lm_head_logprob_grad(x, head, some, 0.8, entropy=True)
+    keep = pick[pick % 2 == 1]
+    _check_on_gpu(x[keep], head, td[keep], 0.8, [a[keep] for a in part], ("half", M, V, H))
+    assert all(not bool(a[::2].any()) for a in part)
+
+
+@pytest.mark.parametrize("M", [3, 70, 300])
+def test_a_head_of_more_than_4_gib(M):
+    V, H = 140000, 16384
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    W = torch.empty((V, H), dtype=torch.bfloat16, device="cuda")
+    for a in range(0, V, 20000):
+        W[a:a + 20000] = torch.randn((min(20000, V - a), H), generator=gen, device="cuda") * 0.01
+    t = torch.randint(0, V, (M,), generator=gen, device="cuda")
+    t[0] = V - 1
+    x = (torch.randn((M, H), generator=gen, device="cuda") + 0.06 * torch.rand((M, 1), generator=gen, device="cuda") * W[t].float() / 0.01).to(torch.bfloat16)
+    head = qerl.lm_head_prepack(W)
+    _check_on_gpu(x, head, t, 1.0, qerl.lm_head_logprob(x, head, t, entropy=True), ("4 GiB", M))
+    _check_on_gpu(x, head, t, 1.0, qerl.lm_head_logprob_grad(x, head, t, entropy=True), ("4 GiB", M))
+
+
 @pytest.mark.parametrize("M", [5, 40, 150, 600])
 @pytest.mark.parametrize("masked", [0.3, 1.0])
 def test_rows_without_a_loss_and_bad_targets(M, masked):
