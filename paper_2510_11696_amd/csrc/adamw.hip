@@ -19,7 +19,9 @@
 // The random bits are a pure function of (seed, t, index): group b of eight elements of the state takes the four words of Philox4x32
 // with 10 rounds, counter (b lo, b hi, t lo, t hi), key (seed lo, seed hi); element j the low (even j) or high half of word j / 2.
 //
-// What bounds the step: memory, 30 bytes per element with 32-bit moments, 18.1 with 8-bit ones.
+// What bounds the step: memory, 30 bytes per element with 32-bit moments, 18.1 with 8-bit ones: 68.8 M elements in 349 us (5.9 TB/s), 80.7 M in
+// 245 us (6.0 TB/s); a plain copy of 2 GiB reaches 4.9.  Eight elements per lane, so that 8-bit moments are 8-byte accesses and a block
+// of 32 is four lanes; one workgroup per 2048 elements of one tensor, so that its addresses are uniform.
 #include <math.h>
 #include <stdlib.h>
 #include "common.hpp"
