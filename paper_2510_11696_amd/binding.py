@@ -889,7 +889,9 @@ def _head_call(name, x, head, targets, inv_temperature, entropy, workspace, out)
         extra = [_dev(out[3], torch.float32, "slope"), lds]
     if workspace is None:
         workspace = lm_head_workspace(M, V, H, gradient, x.device)
-    base = workspace.data_ptr()
+    base = _dev(workspace, torch.uint8, "workspace")
+    if not workspace.is_contiguous() or workspace.device != x.device:
+        raise ValueError("workspace must be contiguous and beside x")
     ptr = (base + 255) & ~255
     _check(name, getattr(lib, name)(
         x_ptr, M, H, ldx, _dev(head.weight, torch.bfloat16, "W"), V, ldw, *([head.weight_t.data_ptr()] if gradient else []), t_ptr,

@@ -340,7 +340,8 @@ def test_binding_refusals():
                 lambda: qerl.lm_head_logprob(x, head, td, entropy=True, out=(torch.empty(4, device="cuda"), None, None))):
         with pytest.raises(ValueError):
             bad()
-    for bad in (lambda: qerl.lm_head_logprob(x, head, td.int()), lambda: qerl.lm_head_logprob(x.float(), head, td), lambda: qerl.lm_head_logprob(x, head, t)):
+    for bad in (lambda: qerl.lm_head_logprob(x, head, td.int()), lambda: qerl.lm_head_logprob(x.float(), head, td), lambda: qerl.lm_head_logprob(x, head, t),
+                lambda: qerl.lm_head_logprob(x, head, td, workspace=torch.empty(1 << 20, dtype=torch.uint8))):
         with pytest.raises(TypeError):
             bad()
     with pytest.raises(qerl.QerlError):
