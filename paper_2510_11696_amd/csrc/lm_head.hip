@@ -54,9 +54,10 @@ __global__ __launch_bounds__(kCompactThreads) void head_compact_kernel(const int
 }
 
 // Reference of the first piece: the logit of the token's own row (a lower bound of the largest).  A row without a loss, where such are not
-// left out, gets +inf, which makes its probabilities 0.  Clears the pieces' flags.
-__global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, float* ref, int* flags, int n_flags) {
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < n_flags; i += gridDim.x * 256) flags[i] = 0;
+// left out, gets +inf, which makes its probabilities 0.  Clears the pieces' flags and what
+// raises references.
+__global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, float* ref, uint32_t* clear, int64_t n_clear) {
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n_clear; i += gridDim.x * 256) clear[i] = 0u;
   const int token = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (token >= head_tokens(a)) return;
   const int64_t row = head_row(a, token), target = a.targets[row];
@@ -77,21 +78,6 @@ __global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, f
   }
   sum = wave_sum(sum);
   if (lane == 0) ref[token] = sum * a.scale;
-}
-
-// After a piece: references of the next one, and which token blocks have to compute the piece again.  One wave per token.
-__global__ __launch_bounds__(256) void head_check_kernel(const HeadArgs a, int parts, int tokens_per_flag, float* ref_next, int* flag) {
-  const int lane = threadIdx.x & 63, token = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (token >= head_tokens(a)) return;
-  float top = kNegInf;
-  for (int b = lane; b < parts; b += 64) top = fmaxf(top, a.part[(int64_t)token * a.part_ld + a.part0 + b].top);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  if (lane != 0) return;
-  const float r = a.ref[token];
-  const bool up = top > r + kRaise;
-  ref_next[token] = up ? top : r;
-  if (up) flag[token / tokens_per_flag] = 1;     // (several may write the same)
 }
 
 // Row results from all parts; for the gradient also 1 - p_t and what turns the sums E into sum p W, and the slopes of rows without one
@@ -209,7 +195,7 @@ struct HeadPlan {
   HeadSumsPlan sums;
   bool compact;                                           // rows without a loss are left out of the products
   int64_t tokens, parts, pieces, piece, flags;            // tokens at a time; parts of a row; pieces and their rows, flags of a piece
-  size_t part, target, index, ref, flag, rest, p, acc, bytes;   // offsets
+  size_t part, target, index, ref, clear, rest, p, acc, bytes;  // offsets; clear: of each piece the flags, then what raises references
 };
 
 // Rows of a piece in blocks of `unit`: at most `most`, as few rounds of workgroups as possible over the vocabulary, then as few pieces
@@ -241,7 +227,7 @@ static HeadPlan plan_head(int64_t M, int64_t V, int64_t H, bool gradient) {
     q.pieces = ceil_div(V, q.piece);
     q.sums = plan_head_sums(q.gemm, q.tokens, H, q.piece);
     q.ref = at; at += up((size_t)(q.tokens * (q.pieces + 1)) * 4);
-    q.flag = at; at += up((size_t)(q.flags * q.pieces) * 4);
+    q.clear = at; at += up((size_t)((q.flags + q.tokens) * q.pieces) * 4);
     q.rest = at; at += up((size_t)(2 * q.tokens) * 4);
     q.p = at; at += up((size_t)(q.tokens * q.piece) * 2);
     q.acc = at; at += up(q.sums.bytes);
@@ -281,11 +267,11 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
     return launch_status();
   }
   float* ref = reinterpret_cast<float*>(c.ws + q.ref);
-  int* flags = reinterpret_cast<int*>(c.ws + q.flag);
+  uint32_t* clear = reinterpret_cast<uint32_t*>(c.ws + q.clear);
   float* rest = reinterpret_cast<float*>(c.ws + q.rest);
   float* e_scale = rest + q.tokens;
   float* slope = c.slope + m0 * c.ld_slope;
-  head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref, flags, (int)(q.flags * q.pieces));
+  head_first_ref_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, ref, clear, (q.flags + q.tokens) * q.pieces);
   HeadArgs e = a;
   e.lda = ceil_div(c.V, 64) * 64; e.rows = c.H; e.b = reinterpret_cast<uint16_t*>(c.ws + q.p); e.ldb = q.piece;
   e.acc = reinterpret_cast<float*>(c.ws + q.acc); e.piece_stages = (int)(q.piece / 64);
@@ -293,13 +279,12 @@ static int run_tokens(const HeadCall& c, const HeadPlan& q, int64_t m0, int64_t 
     const int64_t row0 = i * q.piece, rows = c.V - row0 < q.piece ? c.V - row0 : q.piece;
     a.a = c.W + row0 * c.ldw; a.rows = rows; a.row0 = row0; a.part0 = (int)(row0 / q.gemm.part_rows);
     a.p = reinterpret_cast<uint16_t*>(c.ws + q.p); a.ldp = q.piece;
-    a.ref = ref + i * q.tokens; a.ref_next = ref + (i + 1) * q.tokens; a.flag = nullptr;
+    a.ref = ref + i * q.tokens; a.ref_next = ref + (i + 1) * q.tokens; a.again = 0;
+    a.flag = reinterpret_cast<int*>(clear + i * (q.flags + q.tokens)); a.raise = clear + i * (q.flags + q.tokens) + q.flags;
     if (const int s = launch_head_probs(q.gemm, entropies, a, c.st)) return s;
-    head_check_kernel<<<dim3((unsigned)ceil_div(M, 4)), dim3(256), 0, c.st>>>(a, (int)ceil_div(rows, q.gemm.part_rows), q.gemm.tokens,
-                                                                              ref + (i + 1) * q.tokens, flags + i * q.flags);
-    a.flag = flags + i * q.flags;
+    a.again = 1;
     if (const int s = launch_head_probs(q.gemm, entropies, a, c.st)) return s;
-    e.a = c.Wt + row0; e.k = ceil_div(rows, 64) * 64; e.ref = a.ref; e.ref_next = a.ref_next; e.first = i == 0;
+    e.a = c.Wt + row0; e.k = ceil_div(rows, 64) * 64; e.ref = a.ref; e.raise = a.raise; e.ref_next = a.ref_next; e.first = i == 0;
     if (const int s = launch_head_sums(q.gemm, q.sums, e, c.st)) return s;
   }
   head_finish_kernel<<<dim3((unsigned)M), dim3(256), 0, c.st>>>(a, (int)q.parts, place, ref + q.pieces * q.tokens, logprob, lse, entropy, rest, e_scale, slope,

@@ -24,13 +24,26 @@ struct HeadArgs {
   int64_t row0; int part0;                      // a's first row in the vocabulary, its first part
   // pieces (gradient)
   uint16_t* p; int64_t ldp;                     // probabilities 2^(s - ref) of the piece, 0 at the token's own row and beyond the vocabulary
-  const float* ref; const float* ref_next;      // [tokens] the references of this piece and of the next (raised where a logit passed them by far)
-  const int* flag;                              // [token blocks] which compute the piece again, with ref_next; null: first computation
+  const float* ref;                             // [tokens] the references of this piece
+  uint32_t* raise;                              // [tokens] order_key of the largest logit that passed the reference by far, 0: none did
+  int* flag;                                    // [token blocks] where one did
+  float* ref_next;                              // [tokens] references of the next piece, written with the sums
+  int again;                                    // the piece is computed again for the token blocks with a flag, with head_raised_ref
   float* acc;                                   // sums E: [K-part][token block][row block][tile]
   int first;                                    // the sums start here
   int piece_stages;                             // of 64 rows in a whole piece
 };
 __device__ __forceinline__ int head_tokens(const HeadArgs& a) { return a.count ? *a.count : a.M; }
+// Unsigned keys in the order of the floats, all above 0: a maximum over them does not depend on the order of its atomics
+__device__ __forceinline__ uint32_t order_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float head_raised_ref(const HeadArgs& a, int token) {
+  const uint32_t k = a.raise[token];
+  return k ? key_value(k) : a.ref[token];
+}
 __device__ __forceinline__ int head_row(const HeadArgs& a, int token) { return a.index ? a.index[token] : token; }
 
 // the matrix kernels (lm_head_gemm.hip)

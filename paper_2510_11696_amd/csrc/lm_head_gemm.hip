@@ -256,7 +256,13 @@ __device__ __forceinline__ void head_statistics(f32x16 (&acc)[C::RT][C::TT], con
     float s = sum[0] + sum[1], w = weighted[0] + weighted[1];
     s += __shfl_xor(s, 32, 64);
     if (ENTROPY) w += __shfl_xor(w, 32, 64);
-    if (live && kg == 0) a.part[(int64_t)token * a.part_ld + part] = HeadPart{ref, s, w, top};
+    if (live && kg == 0) {
+      a.part[(int64_t)token * a.part_ld + part] = HeadPart{ref, s, w, top};
+      if (PROBS && !a.again && top > ref + kRaise) {
+        atomicMax(a.raise + token, order_key(top));
+        a.flag[token / C::kTokens] = 1;          // (several may write the same)
+      }
+    }
   }
 }
 
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
       const int width = blocks_per_xcd - 4 * group < 4 ? blocks_per_xcd - 4 * group : 4;
       mb = in / width;
       rb = xcd * blocks_per_xcd + 4 * group + in - mb * width;
-      if (rb < row_blocks && !(PROBS && a.flag && !a.flag[mb])) break;
+      if (rb < row_blocks && !(PROBS && a.again && !a.flag[mb])) break;
     }
     return tile;
   };
@@ -327,7 +333,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
       const int token = wm0 + tt * 32 + loop.n32, at = token < M ? token : M - 1;
       const int64_t far = a.targets[head_row(a, at)] - a.row0 - (r0 + loop.wr * C::RT * 32);
       of[tt].own = far >= 0 && far < 32 * C::RT && (((int)far >> 2) & 1) == loop.kg ? (int)far - 4 * loop.kg : -1;
-      if constexpr (PROBS) of[tt].ref = (a.flag ? a.ref_next : a.ref)[at];
+      if constexpr (PROBS) of[tt].ref = a.again ? head_raised_ref(a, at) : a.ref[at];
     }
     loop.start(0, stages);
   };
@@ -454,8 +460,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
 #pragma unroll
   for (int tt = 0; tt < C::TT; ++tt) {
     int token = m0 + (loop.wt * C::TT + tt) * 32 + loop.n32;
-    token = token < M ? token : M - 1;
-    const float r = a.ref[token], rn = a.ref_next[token], alpha = r == rn ? 1.f : __builtin_amdgcn_exp2f(r - rn);
+    const bool live = token < M;
+    token = live ? token : M - 1;
+    const float r = a.ref[token], rn = head_raised_ref(a, token), alpha = r == rn ? 1.f : __builtin_amdgcn_exp2f(r - rn);
+    if (u.part == 0 && u.rb == 0 && loop.wr == 0 && loop.kg == 0 && live) a.ref_next[token] = rn;
 #pragma unroll
     for (int t = 0; t < C::RT; ++t)
 #pragma unroll
