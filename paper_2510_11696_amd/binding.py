@@ -834,7 +834,8 @@ class LmHead:
 
     def __init__(self, weight: torch.Tensor, weight_t: Optional[torch.Tensor]):
         self.weight, self.weight_t = weight, weight_t
-        self.V, self.H = weight.shape
+        self.V, self.H, self._ldw = _rows(weight, "W")
+        self.device = weight.device
 
 
 def lm_head_prepack(W: torch.Tensor, gradient: bool = True) -> LmHead:
@@ -864,38 +865,40 @@ def _head_call(name, x, head, targets, inv_temperature, entropy, workspace, out)
     gradient = name == "lm_head_logprob_grad"
     M, H, ldx = _rows(x, "x")
     x_ptr = _dev(x, torch.bfloat16, "x")
-    _here(x.device, "x")
-    V, Hw, ldw = _rows(head.weight, "W")
-    if H != Hw:
+    device = x.device
+    _here(device, "x")
+    if H != head.H:
         raise ValueError("x must have as many columns as the head")
-    if head.weight.device != x.device:
+    if head.device != device:
         raise ValueError("x and the head must be on one device")
     if gradient and head.weight_t is None:
         raise ValueError("the head was packed without its transposed order: lm_head_prepack(W, gradient=True)")
     if out is None:
-        out = [torch.empty((M,), dtype=torch.float32, device=x.device) for _ in range(3 if entropy else 2)]
-        out += [None] * (3 - len(out)) + ([torch.empty((M, H), dtype=torch.float32, device=x.device)] if gradient else [])
-    if len(out) != (4 if gradient else 3):
-        raise ValueError("out must be (logprob, lse, entropy or None%s)" % (", slope" if gradient else ""))
-    if (out[2] is not None) != bool(entropy):
-        raise ValueError("entropy=True and its place in out go together")
-    rows = [_flat(t, torch.float32, M, x.device, n) if t is not None else None for t, n in zip(out, ("logprob", "lse", "entropy"))]
-    t_ptr = _flat(targets, torch.int64, M, x.device, "targets")
-    extra = []
-    if gradient:
-        Ms, Hs, lds = _rows(out[3], "slope")
-        if (Ms, Hs) != (M, H) or out[3].device != x.device:
-            raise ValueError("slope must be [M, H] beside x")
-        extra = [_dev(out[3], torch.float32, "slope"), lds]
+        new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=device)
+        out = (new(M), new(M), new(M) if entropy else None) + ((new(M, H),) if gradient else ())
+        rows = [out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr() if entropy else None]
+        slope = (out[3].data_ptr(), H) if gradient else ()
+    else:
+        if len(out) != (4 if gradient else 3):
+            raise ValueError("out must be (logprob, lse, entropy or None%s)" % (", slope" if gradient else ""))
+        if (out[2] is not None) != bool(entropy):
+            raise ValueError("entropy=True and its place in out go together")
+        rows = [_flat(t, torch.float32, M, device, n) if t is not None else None for t, n in zip(out, ("logprob", "lse", "entropy"))]
+        slope = ()
+        if gradient:
+            Ms, Hs, lds = _rows(out[3], "slope")
+            if (Ms, Hs) != (M, H) or out[3].device != device:
+                raise ValueError("slope must be [M, H] beside x")
+            slope = _dev(out[3], torch.float32, "slope"), lds
     if workspace is None:
-        workspace = lm_head_workspace(M, V, H, gradient, x.device)
+        workspace = lm_head_workspace(M, head.V, H, gradient, device)
     base = _dev(workspace, torch.uint8, "workspace")
-    if not workspace.is_contiguous() or workspace.device != x.device:
+    if not workspace.is_contiguous() or workspace.device != device:
         raise ValueError("workspace must be contiguous and beside x")
     ptr = (base + 255) & ~255
     _check(name, getattr(lib, name)(
-        x_ptr, M, H, ldx, _dev(head.weight, torch.bfloat16, "W"), V, ldw, *([head.weight_t.data_ptr()] if gradient else []), t_ptr,
-        float(inv_temperature), *rows, *extra, ptr, workspace.numel() - (ptr - base), _stream()))
+        x_ptr, M, H, ldx, _dev(head.weight, torch.bfloat16, "W"), head.V, head._ldw, *((head.weight_t.data_ptr(),) if gradient else ()),
+        _flat(targets, torch.int64, M, device, "targets"), inv_temperature, *rows, *slope, ptr, workspace.numel() - (ptr - base), _stream()))
     return tuple(out)
 
 
