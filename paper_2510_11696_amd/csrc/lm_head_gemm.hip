@@ -107,8 +107,26 @@ struct HeadLoop {
       if (i >= C::kDeep - C::SA) fetch_a();
     }
   }
-  // Stages from s0 on (as start was told), added to acc
+  // Stages from s0 on (as start was told), added to acc.  SHORT: chains of four stages, their sums added up with what each addition
+  // rounds off (see Head32).
+  template <bool SHORT>
   __device__ __forceinline__ void run(f32x16 (&acc)[C::RT][C::TT], int s0) {
+    float high[SHORT ? C::RT * C::TT * 16 : 1], low[SHORT ? C::RT * C::TT * 16 : 1];
+    if constexpr (SHORT) {
+#pragma unroll
+      for (int i = 0; i < C::RT * C::TT * 16; ++i) high[i] = low[i] = 0.f;
+    }
+    auto add_up = [&] {
+      if constexpr (SHORT) {
+#pragma unroll
+        for (int i = 0; i < C::RT * C::TT * 16; ++i) {
+          const float x = acc[i / 16 / C::TT][i / 16 % C::TT][i % 16], h = high[i], sum = h + x, part = sum - h;
+          low[i] += (h - (sum - part)) + (x - part);
+          high[i] = sum;
+          acc[i / 16 / C::TT][i / 16 % C::TT][i % 16] = 0.f;
+        }
+      }
+    };
     const int full = (int)(k >> 6);              // stages from here on take the tail's way
     auto meet = [&](int s) {                     // everybody has read stage s - 1, and stage s is in LDS
       if (s + C::kDeep - 2 < (s1 < full ? s1 : full)) lds_wait_barrier<C::kAhead>();
@@ -185,6 +203,7 @@ struct HeadLoop {
       put_b = put_b + C::kSlabB == C::SB * C::kSlabB ? 0 : put_b + C::kSlabB;
       slot_a = after_a;
       slot_b = after_b;
+      if (SHORT && ((s - s0) & 3) == 3) add_up();
     }
     for (; s < s1; ++s) {
       three_steps();
@@ -198,6 +217,12 @@ struct HeadLoop {
       __builtin_amdgcn_sched_barrier(0);
       slot_a = after_a;
       slot_b = after_b;
+      if (SHORT && ((s - s0) & 3) == 3) add_up();
+    }
+    if constexpr (SHORT) {
+      add_up();
+#pragma unroll
+      for (int i = 0; i < C::RT * C::TT * 16; ++i) acc[i / 16 / C::TT][i / 16 % C::TT][i % 16] = high[i] + low[i];
     }
   }
 };
@@ -348,7 +373,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
       for (int tt = 0; tt < C::TT; ++tt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[t][tt][i] = 0.f;
-    loop.run(acc, 0);
+    loop.template run<C::kTokens <= 64>(acc, 0);
     const int64_t wr0 = (int64_t)rb * C::kRows + loop.wr * C::RT * 32;
     const int wm0 = mb * C::kTokens + loop.wt * C::TT * 32, part = a.part0 + rb * C::WR + loop.wr;
     const bool results = loop.active && wr0 < a.rows;
@@ -451,7 +476,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
   loop.active = m0 + loop.wt * C::TT * 32 < M;
   if (s1 > s0) {
     loop.start(s0, s1);
-    loop.run(acc, s0);
+    loop.template run<false>(acc, s0);
   }
   if (!loop.active) return;
   // partial sums stay in the registers' order: lane after lane, four rows of a token each
@@ -518,6 +543,9 @@ __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadA
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
+// Up to 64 tokens the logits' products are in chains of 256 inputs: a row whose token is nearly certain has a log-probability that is off, relative
+// to itself, by what its logit is off, and with few rows no other hides it (one chain over 3584 inputs: 3e-6 of a log-probability near 0,
+// in chains 1e-6; the kernels stream the weights either way).
 using Head32 = HeadCfg<2, 1, 2, 1, 4, 4>;        // 128 rows x 32 tokens, two workgroups of two waves per compute unit
 using Head64 = HeadCfg<2, 2, 2, 1, 3, 3>;        // 128 rows x 64 tokens
 using Head128 = HeadCfg<2, 2, 4, 2, 3, 2>;       // 256 rows x 128 tokens
