@@ -898,7 +898,7 @@ def _head_call(name, x, head, targets, inv_temperature, entropy, workspace, out)
     ptr = (base + 255) & ~255
     _check(name, getattr(lib, name)(
         x_ptr, M, H, ldx, _dev(head.weight, torch.bfloat16, "W"), head.V, head._ldw, *((head.weight_t.data_ptr(),) if gradient else ()),
-        _flat(targets, torch.int64, M, device, "targets"), inv_temperature, *rows, *slope, ptr, workspace.numel() - (ptr - base), _stream()))
+        _flat(targets, torch.int64, M, device, "targets"), float(inv_temperature), *rows, *slope, ptr, workspace.numel() - (ptr - base), _stream()))
     return tuple(out)
 
 
@@ -1016,8 +1016,8 @@ def lora_adamw_step(plan: AdamWPlan, lr: Optional[float] = None, step: Optional[
         raise ValueError("give lr or lr_device, and step or step_device")
     _here(plan.device, "the plan")
     one = lambda t, dt, name: _flat(t, dt, 1, plan.device, name) if t is not None else None
-    h = _AdamWHyper(0.0 if lr is None else lr, beta1, beta2, eps, weight_decay, 1 if step is None else step, seed & (2 ** 64 - 1),
-                    one(lr_device, torch.float32, "lr_device"), one(step_device, torch.int64, "step_device"), one(grad_scale, torch.float32, "grad_scale"))
+    h = _AdamWHyper(0.0 if lr is None else float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), 1 if step is None else int(step),
+                    int(seed) & (2 ** 64 - 1), one(lr_device, torch.float32, "lr_device"), one(step_device, torch.int64, "step_device"), one(grad_scale, torch.float32, "grad_scale"))
     _check("lora_adamw_step", load_library().lora_adamw_step(*plan._refs, ctypes.byref(h), _stream()))
 
 
@@ -1027,7 +1027,7 @@ def lora_adamw_grad_norm(plan: AdamWPlan, max_norm: float, out=None):
     _here(plan.device, "the plan")
     norm, scale = out if out is not None else (torch.empty((1,), dtype=torch.float32, device=plan.device) for _ in range(2))
     _check("lora_adamw_grad_norm", load_library().lora_adamw_grad_norm(
-        plan._refs[0], max_norm, _flat(norm, torch.float32, 1, plan.device, "norm"), _flat(scale, torch.float32, 1, plan.device, "scale"), _stream()))
+        plan._refs[0], float(max_norm), _flat(norm, torch.float32, 1, plan.device, "norm"), _flat(scale, torch.float32, 1, plan.device, "scale"), _stream()))
     return norm, scale
 
 

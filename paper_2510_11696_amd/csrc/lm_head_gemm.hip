@@ -9,8 +9,8 @@
 //
 // What bounds it, at that size: the chip's power.  1.26..1.32 PFLOP/s by card with the statistics; the library's product that writes the
 // logits 1.34..1.41.  The matrix pipe is busy 66 % of the cycles, at 1.5..1.9 GHz; leaving out the statistics gains 2 %.  The sums reach
-// 1.29.  Four waves of 128 x 128 take 7.1 ms, eight of 64 x 128 5.2.  Up to 128 tokens it is the head's bytes: 5.9 TB/s at 1 token of
-// 152064 x 3584 (186 us).
+// 1.29.  Four waves of 128 x 128 take 7.1 ms, eight of 64 x 128 5.2.  Up to 128 tokens it is the head's bytes: 5.8 TB/s at 1 token of
+// 152064 x 3584 (188 us).
 //
 // Operand layout in LDS: rows of 64 inputs as eight 16-byte chunks, chunk c of row r at r * 8 + (c ^ ((r >> 1) & 7)).
 #include "lm_head.hpp"
