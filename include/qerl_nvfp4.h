@@ -536,8 +536,8 @@ QERL_API int mxfp4_lora_linear_native(const void* x_bf16, int64_t M, int64_t K, 
  * The head is frozen, as all base weights are.  slope is formed beside the log-probabilities, in one pass over pieces of
  * the vocabulary; a loss then reaches x by lm_head_logprob_backward, dx = bf16(grad_logprob[m] * slope[m]).
  * Sums are fp32, logits the fp32 sums of exact products, logprob = -ln(1 + sum_{v != t} e^(z_v - z_t)), so that it and
- * 1 - p_t keep their relative precision where p_t is near 1; in the sum over v the probabilities enter as bf16 (2^-9
- * relative each).  Results are bit-identical from call to call.
+ * 1 - p_t keep their relative precision where p_t is near 1; in the sum over v the probabilities enter as bf16 (2^-8
+ * relative each at most), but those of 1/32 or more of what all but the token hold together in fp32.  Results are bit-identical from call to call.
  *   x [M, ldx], W [V, ldw] bf16, 16-byte aligned, ld % 8 == 0; H % 8 == 0
  *   Wt: lm_head_prepack_t's output for W (the gradient contracts over the vocabulary; written once, as the weights are frozen)
  *   targets int64 [M].  A target below 0 marks a row without a loss: its logprob, lse, entropy and slope are 0.  One of V or

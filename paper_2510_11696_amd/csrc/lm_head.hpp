@@ -12,6 +12,17 @@ constexpr float kRaise = 60.f;                  // a logit this far (in powers o
 //   ref: what the sums are relative to, sum = sum_others 2^(s - ref), weighted = sum_others 2^(s - ref) (s - ref), top = max_others s
 struct HeadPart { float ref, sum, weighted, top; };
 
+// A probability that holds a large share of what its row's other tokens hold together, and what its rounding to bf16 cut off
+struct HeadLarge { int v; float ref, off, s; };  // vocabulary row; off = 2^(s - ref) less the bf16 value
+constexpr int kLargeSlots = 64;                  // of a token; one per lane
+constexpr float kLargeShare = 1.f / 32;
+struct HeadLargeArgs {
+  HeadLarge* slot; int* count;                   // [tokens][kLargeSlots], [tokens]; once the row results are there, slots hold (v, weight in slope) only
+  float* running;                                // [tokens][2] sum over the pieces so far and what it is relative to
+  int parts, part_rows;                          // of this piece; rows of a part
+  int first;                                     // the piece is the first one
+};
+
 struct HeadArgs {
   const uint16_t* a; int64_t lda, rows;         // row operand [rows, k]: W (rows = vocabulary) or its transpose (rows = hidden)
   const uint16_t* b; int64_t ldb;               // token operand [tokens, k]: x, or the piece's probabilities
@@ -51,11 +62,11 @@ struct HeadGemmPlan { int tokens, rows, part_rows; };   // tokens and vocabulary
 HeadGemmPlan plan_head_gemm(int64_t M, int64_t V, bool gradient);
 int launch_head_logits(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
 int launch_head_probs(const HeadGemmPlan& p, bool entropy, const HeadArgs& a, hipStream_t st);
-// the sums: rows of a tile, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale ] from them
+// the sums: rows of a tile, what the partial sums take; and slope = (1/T) [ (1 - p_t) W_t - sums e_scale - large ones' weights W_v ] from them
 struct HeadSumsPlan { int rows; size_t bytes; };
 HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t piece);
 int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st);
 int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest,
-                      const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st);
+                      const float* e_scale, const HeadLargeArgs& large, float* slope, int64_t ld_slope, hipStream_t st);
 
 }  // namespace qerl

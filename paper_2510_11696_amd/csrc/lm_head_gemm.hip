@@ -505,10 +505,11 @@ __global__ __launch_bounds__(C::kThreads, C::kWaves >= 4 ? C::kWaves / 4 : 1) vo
   }
 }
 
-// slope = (1/T) [ (1 - p_t) W_t - sums e_scale ]; a workgroup takes one row tile of a wave's part of a tile, a wave of it one token tile
+// slope = (1/T) [ (1 - p_t) W_t - sums e_scale - large ones' weights W_v ]; a workgroup takes one row tile of a wave's part of a tile, a wave of it one token tile
 template <class C>
 __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadArgs a, const uint16_t* W, int64_t ldw, int row_blocks, float inv_temperature,
-                                                                     const float* rest, const float* e_scale, float* slope, int64_t ld_slope) {
+                                                                     const float* rest, const float* e_scale, const HeadLargeArgs large, float* slope,
+                                                                     int64_t ld_slope) {
   const int M = head_tokens(a);
   const int t = blockIdx.x % C::RT, wave = blockIdx.x / C::RT % C::kWaves, tile = blockIdx.x / (C::RT * C::kWaves), rb = tile % row_blocks, mb = tile / row_blocks;
   const int wr = wave % C::WR, wt = wave / C::WR, lane = threadIdx.x & 63, tt = threadIdx.x >> 6;
@@ -528,16 +529,28 @@ __global__ __launch_bounds__(64 * C::TT) void head_tile_slope_kernel(const HeadA
   for (int z = 0; z < split; ++z)
 #pragma unroll
     for (int q = 0; q < 4; ++q) s[q] += in[z * slab + q * 64];
+  f32x4 back[4] = {};                            // what the large probabilities' roundings cut off
+  for (int i = 0, n = large.count[token]; i < n; ++i) {
+    const HeadLarge l = large.slot[(int64_t)token * kLargeSlots + i];
+    const uint16_t* wl = W + l.v * ldw + h0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (h0 + 8 * q < a.rows) {
+        const u32x2 wv = *reinterpret_cast<const u32x2*>(wl + 8 * q);
+        back[q] += l.off * f32x4{bf16_bits_to_f32(wv[0] & 0xffffu), __uint_as_float(wv[0] & 0xffff0000u), bf16_bits_to_f32(wv[1] & 0xffffu),
+                                 __uint_as_float(wv[1] & 0xffff0000u)};
+      }
+  }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int64_t h = h0 + 8 * q;
     if (h >= a.rows) break;                      // H is a multiple of 8: four rows are inside or beyond
     const u32x2 wv = *reinterpret_cast<const u32x2*>(w + h);
     f32x4 o;
-    o[0] = bf16_bits_to_f32(wv[0] & 0xffffu) * r - s[q][0] * es;
-    o[1] = __uint_as_float(wv[0] & 0xffff0000u) * r - s[q][1] * es;
-    o[2] = bf16_bits_to_f32(wv[1] & 0xffffu) * r - s[q][2] * es;
-    o[3] = __uint_as_float(wv[1] & 0xffff0000u) * r - s[q][3] * es;
+    o[0] = bf16_bits_to_f32(wv[0] & 0xffffu) * r - s[q][0] * es - back[q][0] * inv_temperature;
+    o[1] = __uint_as_float(wv[0] & 0xffff0000u) * r - s[q][1] * es - back[q][1] * inv_temperature;
+    o[2] = bf16_bits_to_f32(wv[1] & 0xffffu) * r - s[q][2] * es - back[q][2] * inv_temperature;
+    o[3] = __uint_as_float(wv[1] & 0xffff0000u) * r - s[q][3] * es - back[q][3] * inv_temperature;
     *reinterpret_cast<f32x4*>(out + h) = o;
   }
 }
@@ -640,11 +653,11 @@ HeadSumsPlan plan_head_sums(const HeadGemmPlan& p, int64_t M, int64_t H, int64_t
 }
 
 template <class C>
-static int launch_slope(const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale, float* slope, int64_t ld_slope,
-                        hipStream_t st) {
+static int launch_slope(const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest, const float* e_scale, const HeadLargeArgs& large,
+                        float* slope, int64_t ld_slope, hipStream_t st) {
   const int row_blocks = (int)ceil_div(sums.rows, C::kRows);
   head_tile_slope_kernel<C><<<dim3((unsigned)(row_blocks * ceil_div(sums.M, C::kTokens) * C::kWaves * C::RT)), dim3(64 * C::TT), 0, st>>>(
-      sums, head.a, head.lda, row_blocks, inv_temperature, rest, e_scale, slope, ld_slope);
+      sums, head.a, head.lda, row_blocks, inv_temperature, rest, e_scale, large, slope, ld_slope);
   return launch_status();
 }
 int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& a, hipStream_t st) {
@@ -655,12 +668,12 @@ int launch_head_sums(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArg
                            : launch_sums<Head256>(a, st);
 }
 int launch_head_slope(const HeadGemmPlan& p, const HeadSumsPlan& q, const HeadArgs& sums, const HeadArgs& head, float inv_temperature, const float* rest,
-                      const float* e_scale, float* slope, int64_t ld_slope, hipStream_t st) {
-  return p.tokens == 64    ? launch_slope<Head64>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-         : p.tokens == 128 ? launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-         : q.rows == 128   ? launch_slope<HeadHalf>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-         : q.rows == 320   ? launch_slope<Head320>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st)
-                           : launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, slope, ld_slope, st);
+                      const float* e_scale, const HeadLargeArgs& large, float* slope, int64_t ld_slope, hipStream_t st) {
+  return p.tokens == 64    ? launch_slope<Head64>(sums, head, inv_temperature, rest, e_scale, large, slope, ld_slope, st)
+         : p.tokens == 128 ? launch_slope<Head128>(sums, head, inv_temperature, rest, e_scale, large, slope, ld_slope, st)
+         : q.rows == 128   ? launch_slope<HeadHalf>(sums, head, inv_temperature, rest, e_scale, large, slope, ld_slope, st)
+         : q.rows == 320   ? launch_slope<Head320>(sums, head, inv_temperature, rest, e_scale, large, slope, ld_slope, st)
+                           : launch_slope<Head256>(sums, head, inv_temperature, rest, e_scale, large, slope, ld_slope, st);
 }
 
 }  // namespace qerl

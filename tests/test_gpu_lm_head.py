@@ -351,3 +351,95 @@ def test_binding_refusals():
     e = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
     got = qerl.lm_head_logprob(e, head, td[:0], entropy=True)
     assert got[0].shape == (0,)
+
+
+def _slope_bound(x, W, t, inv_t):
+    """(slope, tolerance) where a probability of 1/32 or more of what all but the row's own token hold enters the sum in fp32: only the others carry the
+    2^-8 of bf16 in the bound at the top of this file."""
+    x, W = x.double().cpu().numpy(), W.double().cpu().numpy()
+    (M, H), V = x.shape, W.shape[0]
+    z = inv_t * (x @ W.T)
+    D = (2 * ((H / 16 + 24) * U * inv_t * (np.abs(x) @ np.abs(W).T).max(1) + 4 * U * np.abs(z).max(1)))[:, None]
+    _, lse, _, slope = uo.head_logprob(x, W, t, inv_t)
+    p = np.exp(z - lse[:, None])
+    p[np.arange(M), t] = 0
+    rest = p.sum(1, keepdims=True)
+    small = np.where(p >= rest / 32, 0, p)
+    return slope, inv_t * ((D + 2.0 ** -16) * rest * np.abs(W[t]) + (D + 2.0 ** -16 + (V / 16 + 64) * U) * (p @ np.abs(W)) + 2.0 ** -8 * (small @ np.abs(W)))
+
+
+def _check_slope(slope, x, W, t, inv_t, what):
+    want, tol = _slope_bound(x, W, t, inv_t)
+    off = np.abs(slope.double().cpu().numpy() - want) - tol
+    assert np.all(off <= 0), (what, float((off + tol).max()), float((off / tol).max()), np.argwhere(~(off <= 0))[:4].tolist())
+    return want, tol
+
+
+@pytest.mark.parametrize("together", [1, 2, 5])
+@pytest.mark.parametrize("M,V,H,inv_t", [(1, 300, 64, 1.0), (40, 5000, 256, 1.0), (100, 3001, 136, 0.7), (300, 2000, 264, 1.0), (700, 4099, 128, 1.25)])
+def test_rows_whose_mass_is_on_other_tokens(M, V, H, inv_t, together):
+    """An unlikely token was sampled: one, two or five neighbouring others hold nearly all of the mass, at the vocabulary's ends and across the
+    borders of tiles among them.  The slope there is little but a few rows of W, so that nothing averages a rounding of their probabilities."""
+    print("dominated case", M, V, H, inv_t, together, flush=True)
+    x, W, t = _inputs(M, V, H, 500 + M, sure=0.0)
+    g = torch.Generator().manual_seed(M + together)
+    u = torch.randint(0, V - together, (M,), generator=g)
+    u[: min(M, 6)] = torch.tensor([V - together, 0, 62, 126, 254, 1022 % (V - together)])[: min(M, 6)]
+    t = torch.where((t >= u) & (t < u + together), (u + together + 1) % V, t)
+    Wf = W.float().cpu()
+    xf = x.float().cpu()
+    for i in range(together):
+        w = Wf[u + i]
+        xf += (11.0 + 3 * torch.rand((M, 1), generator=g)) / inv_t * w / (w * w).sum(1, keepdim=True)
+    x.copy_(xf.to(torch.bfloat16))
+    head = qerl.lm_head_prepack(W)
+    got = qerl.lm_head_logprob_grad(x, head, t.cuda(), inv_t, entropy=True)
+    want, tol = _check_slope(got[3], x, W, t.numpy(), inv_t, (M, V, H, together))
+    # the bound is one that a rounding of the large ones to bf16 (2^-10 of the slope in the mean) would not meet
+    assert np.median(np.linalg.norm(tol, axis=1) / np.linalg.norm(want, axis=1)) < 2.0 ** -10
+    ref, all_tol = _bounds(x, W, t.numpy(), inv_t, H, V)
+    _check(got, ref, all_tol, slice(None), ("dominated", M, V, H))
+    # some rows without a loss among them; the others bit for bit, up to the order of sums where rows are left out
+    some = t.clone()
+    some[::3] = -1
+    part = qerl.lm_head_logprob_grad(x, head, some.cuda(), inv_t)[3]
+    keep = np.arange(M) % 3 != 0
+    if keep.any():
+        _check_slope(part[torch.from_numpy(keep)], x[torch.from_numpy(keep)], W, t.numpy()[keep], inv_t, ("masked", M, V, H, together))
+    assert not bool(part[::3].any())
+
+
+@pytest.mark.parametrize("levels", [(0, 0, 0, 0, 0), (0, 3, 6, 9, 12), (12, 9, 6, 3, 0), (0, 3, 80, 83, 90)])
+def test_large_probabilities_of_several_pieces(levels):
+    """8200 rows take the vocabulary in five pieces.  25 tokens in nearly equal parts stand out in each of the first four, three in the last, `levels`
+    above one another: where the levels rise, more are large on the way than are kept, and the three have to stay; with a step of 77 references
+    are raised in between."""
+    M, V, H = 8200, 60000, 64
+    g = torch.Generator().manual_seed(levels[0] + levels[4])
+    d = torch.randn((H,), generator=g)
+    d /= d.norm()
+    W = torch.randn((V, H), generator=g) * 0.05
+    for a, n, level in zip((100, 14000, 26000, 40000, V - 3), (25, 25, 25, 25, 3), levels):
+        apart = torch.randn((n, H), generator=g) * 0.3
+        W[a:a + n] = d * (12 + level) / 8 + apart - (apart @ d)[:, None] * d
+    W = W.to(torch.bfloat16).cuda()
+    x = (8 * d + torch.randn((M, H), generator=g) * 0.02).to(torch.bfloat16).cuda()
+    t = torch.randint(200, 13000, (M,), generator=g)
+    slope = qerl.lm_head_logprob_grad(x, qerl.lm_head_prepack(W), t.cuda())[3]
+    rows = np.r_[0:30, 4000:4030, 8170:8200]
+    _check_slope(slope[rows], x[rows], W, t.numpy()[rows], 1.0, levels)
+
+
+def test_a_large_probability_beside_a_token_that_is_nearly_certain():
+    """1 - p_t is small and one other token holds nearly all of it: the slope, small as a whole, keeps its relative precision."""
+    M, V, H = 90, 2500, 256
+    x, W, t = _inputs(M, V, H, 41, sure=0.0)
+    u = (t + 700) % V
+    Wf, xf = W.float().cpu(), x.float().cpu()
+    for at, z in ((t, 30.0), (u, 14.0)):
+        w = Wf[at]
+        xf += z * w / (w * w).sum(1, keepdim=True)
+    x.copy_(xf.to(torch.bfloat16))
+    got = qerl.lm_head_logprob_grad(x, qerl.lm_head_prepack(W), t.cuda())
+    assert float(got[0].median()) > -1e-3
+    _check_slope(got[3], x, W, t.numpy(), 1.0, "sure")
