@@ -120,6 +120,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
     const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
     if (step < 1 || !(lr >= 0.0) || !isfinite(lr)) return;   // what the host refuses
     const AdamFactors f = adam_factors(lr, a.beta1, a.beta2, a.wd, step);
+    if (!isfinite(f.decay) || !isfinite(f.step_size)) return;
     decay = f.decay; step_size = f.step_size; isb2 = f.isb2;
   }
   const uint32_t chunk = blockIdx.x;
@@ -412,24 +413,24 @@ extern "C" int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_sta
   if (const int e = state_status(state, plan->elements)) return e;
   if (!h) return QERL_ERR_NULL;
   const bool lr_ok = h->lr_device || (isfinite(h->lr) && h->lr >= 0), step_ok = h->step_device || h->step >= 1;
-  if (!lr_ok || !step_ok || !(h->beta1 >= 0 && h->beta1 < 1) || !(h->beta2 >= 0 && h->beta2 < 1) || !(h->eps > 0 && isfinite(h->eps)) ||
+  const float eps = (float)h->eps;                       // as the kernel adds it: 0 would make 0 / 0 of every element without a gradient
+  if (!lr_ok || !step_ok || !(h->beta1 >= 0 && h->beta1 < 1) || !(h->beta2 >= 0 && h->beta2 < 1) || !(eps > 0 && isfinite(eps)) ||
       !(h->weight_decay >= 0 && isfinite(h->weight_decay)))
     return QERL_ERR_SHAPE;
+  const bool dev = h->lr_device || h->step_device;
+  const AdamFactors f = dev ? AdamFactors{} : adam_factors(h->lr, h->beta1, h->beta2, h->weight_decay, h->step);
+  if (!isfinite(f.decay) || !isfinite(f.step_size)) return QERL_ERR_SHAPE;
   if (!aligned(h->lr_device, 4) || !aligned(h->step_device, 8) || !aligned(h->grad_scale, 4)) return QERL_ERR_ALIGN;
   if (plan->chunks == 0) return QERL_OK;
   AdamArgs a = {};
   a.table = tensors_of(plan);
   a.owner = owner_of(plan);
   a.m = state->m; a.v = state->v; a.ms = state->m_scale; a.vs = state->v_scale;
-  a.b1 = (float)h->beta1; a.omb1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.omb2 = (float)(1.0 - h->beta2); a.eps = (float)h->eps;
+  a.b1 = (float)h->beta1; a.omb1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.omb2 = (float)(1.0 - h->beta2); a.eps = eps;
   a.lr = h->lr; a.beta1 = h->beta1; a.beta2 = h->beta2; a.wd = h->weight_decay; a.step = h->step;
   a.lr_dev = h->lr_device; a.step_dev = h->step_device; a.grad_scale = h->grad_scale;
   a.k0 = (uint32_t)h->seed; a.k1 = (uint32_t)(h->seed >> 32);
-  const bool dev = h->lr_device || h->step_device;
-  if (!dev) {
-    const AdamFactors f = adam_factors(h->lr, h->beta1, h->beta2, h->weight_decay, h->step);
-    a.decay = f.decay; a.step_size = f.step_size; a.isb2 = f.isb2;
-  }
+  a.decay = f.decay; a.step_size = f.step_size; a.isb2 = f.isb2;
   const dim3 grid((unsigned)plan->chunks), block(kAdamThreads);
   hipStream_t st = (hipStream_t)stream;
   if (state->bits == 8) {

@@ -158,3 +158,19 @@ def test_binding_refuses_cpu_tensors():
         qerl.lm_head_logprob_backward(torch.zeros(4), torch.zeros((4, 64)))
     with pytest.raises(ValueError):
         qerl.lora_adamw_plan([], [])
+
+
+def _step(lib, **kw):
+    h = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=1, seed=0, lr_device=None, step_device=None, grad_scale=None)
+    h.update(kw)
+    pl, st = _AdamWPlanStruct(FAKE, 1024, 0, 1), _AdamWState(8, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE)      # no pieces: nothing is launched
+    return lib.lora_adamw_step(ctypes.byref(pl), ctypes.byref(st), ctypes.byref(_AdamWHyper(*h.values())), None)
+
+
+def test_adamw_numbers_that_fp32_does_not_hold(lib):
+    """What the kernel computes with are the numbers as fp32: an eps that rounds to 0 would leave 0 / 0 wherever there has been no gradient."""
+    for kw in (dict(eps=1e-46), dict(eps=1e300), dict(lr=1e39), dict(lr=1e38, beta1=0.9), dict(lr=1e20, weight_decay=1e30), dict(lr=1e300, weight_decay=1e300)):
+        assert _step(lib, **kw) == SHAPE, kw
+    for kw in (dict(eps=1e-45), dict(eps=3e38), dict(lr=3e37), dict(lr=0.0, weight_decay=1e30), dict(lr=1e8, weight_decay=1e30),
+               dict(beta1=1 - 2.0 ** -53, beta2=1 - 2.0 ** -53), dict(lr=1e-3, beta1=0.0, step=2 ** 62)):
+        assert _step(lib, **kw) == 0, kw

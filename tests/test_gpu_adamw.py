@@ -311,3 +311,31 @@ def test_update_of_a_policy_with_the_operators_around_its_linears():
     ref = oracle.nvfp4_lora_linear(x.float().cpu().numpy(), codes, scales, ts, A.float().cpu().numpy(), B.float().cpu().numpy(), scale)
     from tests.gpu_util import check_linear
     check_linear(y2, ref, "after the step")
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_captured_values_whose_factors_fp32_does_not_hold_change_nothing(bits):
+    s = _Set([500], bits, 2, copies=False)
+    s.gradients()
+    lr, step = torch.tensor([3e38], device="cuda"), torch.tensor([1], device="cuda")
+    for kw in (dict(beta1=0.9), dict(beta1=0.0, weight_decay=10.0)):                     # lr / (1 - b1^t), 1 - lr wd
+        qerl.lora_adamw_step(s.plan, lr_device=lr, step_device=step, **kw)
+        s.check()
+    lr.fill_(HYPER["lr"])                                                                # the same step counts once they can be held
+    s.reference(1, 0, **{**HYPER, "lr": lr.item()})
+    qerl.lora_adamw_step(s.plan, lr_device=lr, step_device=step, **{k: v for k, v in HYPER.items() if k != "lr"})
+    s.check()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_the_smallest_eps_leaves_elements_without_a_gradient(bits):
+    s = _Set([300], bits, 3)
+    s.g = [np.zeros(300, np.float32)]
+    s.gg[0].zero_()
+    h = {**HYPER, "eps": 1e-45}
+    qerl.lora_adamw_step(s.plan, step=1, seed=1, **h)
+    s.reference(1, 1, **h)
+    s.check()
+    assert np.all(np.isfinite(s.p[0]))
+    with pytest.raises(qerl.QerlError):
+        qerl.lora_adamw_step(s.plan, step=2, seed=1, **{**HYPER, "eps": 1e-46})
