@@ -585,6 +585,8 @@ QERL_API int lm_head_logprob_backward(const float* grad_logprob_f32, const float
  *   (to nearest, 0.1 and 0.001 of a moment would not move it), by 16 random bits per element:
  *   Philox4x32 with 10 rounds, counter (b lo, b hi, t lo, t hi), key (seed lo, seed hi), b the group of eight state elements,
  *   element j of it the low (even j) or high half of word j / 2.  Zero-filled memory is the state before the first step.
+ *   Its memory must be apart from the tensors' and the table's: lora_adamw_check_state says whether a state fits a list of tensors and (if not
+ *   NULL) a table, once and on the host (the other calls, which take the plan only, check the state's parts against each other).
  * lora_adamw_step: one step.  hyper is a HOST struct.  lr_device, step_device and grad_scale are device pointers or NULL:
  *   *lr_device and *step_device, where given, are read in place of lr and step when the launch runs, so that a captured
  *   step can be replayed with another rate and step count.  If *grad_scale or *lr_device is not finite, *lr_device is
@@ -594,7 +596,7 @@ QERL_API int lm_head_logprob_backward(const float* grad_logprob_f32, const float
  *   The sums of its workgroups pass through the table, so norms of one plan must be ordered on one stream, as its steps must.
  * lora_adamw_moments: the values of an 8-bit state as fp32, m and v [state elements] (inspection, checkpoints).
  * Errors: NULL pointers (copy_bf16 may be NULL); n < 0, n_tensors outside 1..2^20, more than 2^31 - 1 pieces of 2048
- * elements, memory that a step writes named twice (tensors or parts of the state), bits other than 8 and 32, step < 1, lr, weight_decay < 0 or not
+ * elements, memory that a step writes named twice (tensors, table or, where they are checked, parts of the state), bits other than 8 and 32, step < 1, lr, weight_decay < 0 or not
  * finite, betas outside [0, 1), eps that is 0 or less or not finite, eps and factors (1 - lr wd, lr / (1 - b1^t)) as fp32 (QERL_ERR_SHAPE); parameters, gradients, copies, m or v not 16-byte aligned
  * (QERL_ERR_ALIGN); table too small or misaligned (QERL_ERR_WORKSPACE).
  */
@@ -628,6 +630,7 @@ QERL_API size_t lora_adamw_plan_bytes(const qerl_adamw_tensor* tensors, int n_te
 QERL_API int64_t lora_adamw_state_elements(const qerl_adamw_tensor* tensors, int n_tensors);       /* host; -1 for a bad list */
 QERL_API int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tensors, void* table, size_t table_bytes,
                                   qerl_adamw_plan* plan, void* stream);
+QERL_API int lora_adamw_check_state(const qerl_adamw_tensor* tensors, int n_tensors, const void* table, const qerl_adamw_state* state);   /* host */
 QERL_API int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_state* state, const qerl_adamw_hyper* hyper, void* stream);
 QERL_API int lora_adamw_grad_norm(const qerl_adamw_plan* plan, double max_norm, float* norm_f32, float* scale_f32, void* stream);
 QERL_API int lora_adamw_moments(const qerl_adamw_plan* plan, const qerl_adamw_state* state, float* m_f32, float* v_f32, void* stream);

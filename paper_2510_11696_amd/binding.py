@@ -87,6 +87,7 @@ _SIGNATURES = {
     "lora_adamw_plan_bytes": (_c_sz, [_c_p, ctypes.c_int]),
     "lora_adamw_state_elements": (_c_i64, [_c_p, ctypes.c_int]),
     "lora_adamw_make_plan": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_sz, _c_p, _c_p]),
+    "lora_adamw_check_state": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_p]),
     "lora_adamw_step": (ctypes.c_int, [_c_p, _c_p, _c_p, _c_p]),
     "lora_adamw_grad_norm": (ctypes.c_int, [_c_p, ctypes.c_double, _c_p, _c_p, _c_p]),
     "lora_adamw_moments": (ctypes.c_int, [_c_p, _c_p, _c_p, _c_p, _c_p]),
@@ -959,19 +960,17 @@ class AdamWPlan:
     them; every step reads the gradients from the tensors given here, so the backward pass has to write those (its `dA` and `dB`
     arguments, or a copy)."""
 
-    def __init__(self, struct, table, tensors, bits, m, v, m_scale, v_scale):
-        self.struct, self.table, self.tensors, self.bits = struct, table, tensors, bits
+    def __init__(self, struct, table, tensors, moments, m, v, m_scale, v_scale):
+        self.struct, self.table, self.tensors, self.bits = struct, table, tensors, moments.bits
         self.m, self.v, self.m_scale, self.v_scale = m, v, m_scale, v_scale
         self.elements, self.device = int(struct.elements), table.device
-        self._state = _AdamWState(bits, m.data_ptr(), v.data_ptr(), m_scale.data_ptr() if bits == 8 else None,
-                                  v_scale.data_ptr() if bits == 8 else None)
-        self._refs = ctypes.byref(struct), ctypes.byref(self._state)
+        self._refs = ctypes.byref(struct), ctypes.byref(moments)
 
 
 def lora_adamw_plan(params, grads, copies=None, state_bits: int = 8, state=None) -> AdamWPlan:
     """params, grads: lists of contiguous fp32 tensors; copies: None or a list of bf16 tensors (or None) that each step writes
     from the updated parameters; state: None (zeros) or the moments to go on from, (m, v, m_scale, v_scale) as uint8 for 8 bits,
-    (m, v) as fp32 for 32, laid out as the header says."""
+    (m, v) as fp32 for 32, laid out as the header says.  Memory that a step writes (parameters, copies, moments) must not be given twice."""
     lib = load_library()
     n = len(params)
     copies = copies if copies is not None else [None] * n
@@ -1002,8 +1001,10 @@ def lora_adamw_plan(params, grads, copies=None, state_bits: int = 8, state=None)
     m, v, ms, vs = (*state, None, None)[:4]
     table = torch.empty((need,), dtype=torch.uint8, device=device)
     struct = _AdamWPlanStruct()
+    moments = _AdamWState(state_bits, *(t.data_ptr() for t in state))
+    _check("lora_adamw_check_state", lib.lora_adamw_check_state(arr, n, table.data_ptr(), ctypes.byref(moments)))
     _check("lora_adamw_make_plan", lib.lora_adamw_make_plan(arr, n, table.data_ptr(), table.numel(), ctypes.byref(struct), _stream()))
-    return AdamWPlan(struct, table, (list(params), list(grads), list(copies)), state_bits, m, v, ms, vs)
+    return AdamWPlan(struct, table, (list(params), list(grads), list(copies)), moments, m, v, ms, vs)
 
 
 def lora_adamw_step(plan: AdamWPlan, lr: Optional[float] = None, step: Optional[int] = None, beta1: float = 0.9, beta2: float = 0.999,

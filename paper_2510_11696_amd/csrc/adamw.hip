@@ -297,11 +297,13 @@ static int by_begin(const void* a, const void* b) {
   const uintptr_t x = static_cast<const Span*>(a)->begin, y = static_cast<const Span*>(b)->begin;
   return x < y ? -1 : x > y;
 }
-// 0, 1 if memory that a step writes is named twice, -1 if the list of spans could not be held
-static int overlaps(const qerl_adamw_tensor* t, int n) {
-  Span* s = static_cast<Span*>(malloc(sizeof(Span) * 3 * (size_t)n));
+// 0, 1 if memory that a step writes is named twice among the tensors and what else is written, -1 if the list of spans could not be held
+static int overlaps(const qerl_adamw_tensor* t, int n, const Span* others, int n_others) {
+  Span* s = static_cast<Span*>(malloc(sizeof(Span) * (3 * (size_t)n + n_others)));
   if (!s) return -1;
   size_t k = 0;
+  for (int i = 0; i < n_others; ++i)
+    if (others[i].end > others[i].begin) s[k++] = others[i];
   for (int i = 0; i < n; ++i) {
     if (t[i].n == 0) continue;
     const uintptr_t p = (uintptr_t)t[i].param_f32, c = (uintptr_t)t[i].copy_bf16, g = (uintptr_t)t[i].grad_f32;
@@ -370,9 +372,11 @@ extern "C" int lora_adamw_make_plan(const qerl_adamw_tensor* tensors, int n_tens
     if (!t.param_f32 || !t.grad_f32) return QERL_ERR_NULL;
     if (!aligned(t.param_f32, 16) || !aligned(t.grad_f32, 16) || !aligned(t.copy_bf16, 16)) return QERL_ERR_ALIGN;
   }
-  if (const int o = overlaps(tensors, n_tensors)) return o > 0 ? QERL_ERR_SHAPE : QERL_ERR_WORKSPACE;
+  if (const int o = overlaps(tensors, n_tensors, nullptr, 0)) return o > 0 ? QERL_ERR_SHAPE : QERL_ERR_WORKSPACE;
   if (!table || table_bytes < l.bytes) return QERL_ERR_WORKSPACE;
   if (!aligned(table, 256)) return QERL_ERR_WORKSPACE;
+  const Span own = {(uintptr_t)table, (uintptr_t)table + l.bytes, 1};
+  if (const int o = overlaps(tensors, n_tensors, &own, 1)) return o > 0 ? QERL_ERR_SHAPE : QERL_ERR_WORKSPACE;
   AdamTensor* out = reinterpret_cast<AdamTensor*>(static_cast<uint8_t*>(table) + kNormBytes);
   TableBatch batch = {};
   int64_t state0 = 0, chunk0 = 0;
@@ -406,6 +410,19 @@ static int state_status(const qerl_adamw_state* s, int64_t elements) {
                         apart(s->v, n, s->m_scale, b) && apart(s->v, n, s->v_scale, b)))
     return QERL_ERR_SHAPE;
   return QERL_OK;
+}
+
+extern "C" int lora_adamw_check_state(const qerl_adamw_tensor* tensors, int n_tensors, const void* table, const qerl_adamw_state* state) {
+  if (!tensors || !state) return QERL_ERR_NULL;
+  AdamLayout l;
+  if (!adam_layout(tensors, n_tensors, l)) return QERL_ERR_SHAPE;
+  if (const int e = state_status(state, l.elements)) return e;
+  if (l.elements == 0) return QERL_OK;
+  const uintptr_t n = (uintptr_t)l.elements * (state->bits / 8), b = state->bits == 8 ? (uintptr_t)l.elements / kStateBlock : 0;
+  const auto span = [](const void* p, uintptr_t bytes) { return Span{(uintptr_t)p, (uintptr_t)p + bytes, 1}; };
+  const Span others[5] = {span(state->m, n), span(state->v, n), span(state->m_scale, b), span(state->v_scale, b), span(table, table ? l.bytes : 0)};
+  const int o = overlaps(tensors, n_tensors, others, 5);
+  return o == 0 ? QERL_OK : o > 0 ? QERL_ERR_SHAPE : QERL_ERR_WORKSPACE;
 }
 
 extern "C" int lora_adamw_step(const qerl_adamw_plan* plan, const qerl_adamw_state* state, const qerl_adamw_hyper* h, void* stream) {

@@ -174,3 +174,36 @@ def test_adamw_numbers_that_fp32_does_not_hold(lib):
     for kw in (dict(eps=1e-45), dict(eps=3e38), dict(lr=3e37), dict(lr=0.0, weight_decay=1e30), dict(lr=1e8, weight_decay=1e30),
                dict(beta1=1 - 2.0 ** -53, beta2=1 - 2.0 ** -53), dict(lr=1e-3, beta1=0.0, step=2 ** 62)):
         assert _step(lib, **kw) == 0, kw
+
+
+def test_adamw_state_must_be_apart_from_the_tensors(lib):
+    G = 0x100000
+    tensors = [(G, 2 * G, 3 * G, 1000), (4 * G, None, 5 * G, 7), (None, None, None, 0)]     # 1056 state elements
+    arr, table = ctypes.cast(_tensors(tensors), p), 20 * G
+    nbytes = lib.lora_adamw_plan_bytes(arr, 3)
+
+    def check(bits=8, m=10 * G, v=11 * G, ms=12 * G, vs=13 * G, table=table):
+        st = _AdamWState(bits, m, v, ms, vs)
+        return lib.lora_adamw_check_state(arr, 3, table, ctypes.byref(st))
+    assert check() == 0 and check(bits=32) == 0 and check(table=None) == 0
+    for bits in (8, 32):
+        size = 1056 * bits // 8
+        for part in ("m", "v"):
+            # on a parameter, a copy or a gradient: at its start, over its last element, from before into its first
+            for start, length in ((G, 4000), (2 * G, 2000), (3 * G, 4000), (4 * G, 28), (5 * G, 28)):
+                for at in (start, (start + length - 1) // 16 * 16, start - size + 16):
+                    assert check(bits, **{part: at}) == SHAPE, (bits, part, hex(at))
+                assert check(bits, **{part: (start + length + 15) // 16 * 16}) == 0 and check(bits, **{part: (start - size) // 16 * 16}) == 0
+            assert check(bits, **{part: table}) == SHAPE and check(bits, **{part: table + nbytes - 16}) == SHAPE and check(bits, **{part: table + nbytes}) == 0
+            assert check(bits, **{part: table + 16}, table=None) == 0
+    for part in ("ms", "vs"):
+        for at in (G + 3999, 2 * G - 32, 3 * G, table):
+            assert check(**{part: at}) == SHAPE, (part, hex(at))
+        assert check(**{part: G - 33}) == 0 and check(**{part: G + 4000}) == 0 and check(bits=32, **{part: G}) == 0
+    assert check(v=10 * G + 16) == SHAPE and check(bits=16) == SHAPE and check(m=None) == NULL and check(ms=None) == NULL and check(m=10 * G + 8) == ALIGN
+    empty = ctypes.cast(_tensors([(None, None, None, 0)]), p)
+    assert lib.lora_adamw_check_state(empty, 1, table, ctypes.byref(_AdamWState(8, None, None, None, None))) == 0
+    assert lib.lora_adamw_check_state(arr, 0, table, ctypes.byref(_AdamWState(8))) == SHAPE
+    assert lib.lora_adamw_check_state(None, 1, table, ctypes.byref(_AdamWState(8))) == NULL and lib.lora_adamw_check_state(arr, 3, table, None) == NULL
+    # the table of a plan
+    assert _make(lib, tensors, table=3 * G + 3840) == SHAPE and _make(lib, tensors, table=G - 256) == SHAPE

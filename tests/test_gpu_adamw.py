@@ -339,3 +339,25 @@ def test_the_smallest_eps_leaves_elements_without_a_gradient(bits):
     assert np.all(np.isfinite(s.p[0]))
     with pytest.raises(qerl.QerlError):
         qerl.lora_adamw_step(s.plan, step=2, seed=1, **{**HYPER, "eps": 1e-46})
+
+
+def test_a_state_on_memory_of_the_tensors_is_refused():
+    flat = torch.zeros((4096,), device="cuda")
+    cut = lambda a, n: flat[a:a + n]
+    other = lambda n, dt=torch.float32: torch.zeros((n,), dtype=dt, device="cuda")
+    p, g, c = cut(0, 64), cut(64, 64), other(64, torch.bfloat16)
+    byte = flat.view(torch.uint8)
+    for state in ((cut(0, 64), other(64)), (other(64), cut(0, 64)), (cut(64, 64), other(64)), (other(64), cut(100, 64)), (cut(60, 64), other(64))):
+        with pytest.raises(qerl.QerlError):
+            qerl.lora_adamw_plan([p], [g], [c], state_bits=32, state=state)
+    e = lambda n: other(n, torch.uint8)
+    for state in ((byte[240:304], e(64), e(2), e(2)), (e(64), byte[256:320], e(2), e(2)), (e(64), e(64), byte[255:257], e(2)), (e(64), e(64), e(2), byte[511:513]),
+                  (e(64), e(64), e(2), c.view(torch.uint8)[126:128])):
+        with pytest.raises(qerl.QerlError):
+            qerl.lora_adamw_plan([p], [g], [c], state_bits=8, state=state)
+    assert not bool(flat.any())
+    # beside them it works: everything in one buffer
+    g.fill_(1.0)
+    plan = qerl.lora_adamw_plan([p], [g], [c], state_bits=32, state=(cut(128, 64), cut(192, 64)))
+    qerl.lora_adamw_step(plan, lr=1e-3, step=1)
+    assert bool((flat[:64] < 0).all()) and bool((flat[128:256] > 0).all()) and not bool(flat[256:].any())
