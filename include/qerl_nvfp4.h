@@ -326,7 +326,7 @@ QERL_API int nvfp4_lora_linear_packed_swiglu(const void* gate_bf16, const void* 
  *   r == 0: only dX is written (x, A, B, dA, dB may be NULL).
  *   workspace: >= nvfp4_lora_linear_backward_workspace_bytes(M, N, K, r),
  *   256-byte aligned; needs no initialisation.
- * Errors: as the forward functions.
+ * Errors: as the forward functions; QERL_ERR_SHAPE for dA and dB that share memory.
  */
 QERL_API size_t nvfp4_prepack_t_bytes(int64_t N, int64_t K);   /* host */
 QERL_API int nvfp4_prepack_t(const uint8_t* codes, const uint8_t* scales, int64_t N, int64_t K,
@@ -358,7 +358,8 @@ QERL_API int nvfp4_lora_linear_backward(const void* x_bf16, const void* dy_bf16,
  *   workspace: >= nvfp4_lora_linear_backward_group_workspace_bytes(M, K, members,
  *            n_members) (0 for n_members outside 1..4), 256-byte aligned; needs
  *            no initialisation.
- * Errors: as nvfp4_lora_linear_backward; QERL_ERR_SHAPE for n_members outside 1..4.
+ * Errors: as nvfp4_lora_linear_backward; QERL_ERR_SHAPE for n_members outside 1..4 and for gradients (dA_i, dB_i of all members) that
+ * share memory.
  */
 typedef struct {
   const void* dy_bf16;         /* [M, lddy] upstream gradient of this member's output */

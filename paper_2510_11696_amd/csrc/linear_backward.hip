@@ -403,6 +403,21 @@ static int backward_validate(const void* x, int64_t M, int64_t K, int64_t ldx, c
   return QERL_OK;
 }
 
+// No two of the gradients on the same memory: the members' products are written by one launch
+static bool gradients_apart(const BackwardMember* mem, int n, int64_t K) {
+  struct { uintptr_t begin, end; } s[2 * kMaxGroup];
+  int k = 0;
+  for (int i = 0; i < n; ++i) {
+    if (mem[i].r == 0) continue;
+    s[k].begin = (uintptr_t)mem[i].dA; s[k].end = s[k].begin + 4 * (uintptr_t)(mem[i].r * K); ++k;
+    s[k].begin = (uintptr_t)mem[i].dB; s[k].end = s[k].begin + 4 * (uintptr_t)(mem[i].r * mem[i].N); ++k;
+  }
+  for (int i = 0; i < k; ++i)
+    for (int j = 0; j < i; ++j)
+      if (s[i].begin < s[j].end && s[j].begin < s[i].end) return false;
+  return true;
+}
+
 // A call's launches: one that transposes all adapters, per member a down-projection of its own dY, the
 // down-projections of x (one launch over all adapters), dX -- ONE GEMM whose contraction runs over the members' rows one
 // after the other, so that dX is summed in fp32 and rounded once -- and one or two for the gradient products of all
@@ -413,6 +428,7 @@ static int backward_run(const uint16_t* x, int64_t M, int64_t K, int64_t ldx, co
   for (int i = 0; i < n; ++i) { Ns[i] = mem[i].N; rs[i] = mem[i].r; }
   const BackwardLayout L = backward_layout(M, K, Ns, rs, n);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < L.total) return QERL_ERR_WORKSPACE;
+  if (!gradients_apart(mem, n, K)) return QERL_ERR_SHAPE;
   uint8_t* ws = (uint8_t*)workspace;
   uint32_t* counters = (uint32_t*)(ws + L.ctr_off);
   float* part = (float*)(ws + L.part_off);

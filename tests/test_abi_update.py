@@ -207,3 +207,27 @@ def test_adamw_state_must_be_apart_from_the_tensors(lib):
     assert lib.lora_adamw_check_state(None, 1, table, ctypes.byref(_AdamWState(8))) == NULL and lib.lora_adamw_check_state(arr, 3, table, None) == NULL
     # the table of a plan
     assert _make(lib, tensors, table=3 * G + 3840) == SHAPE and _make(lib, tensors, table=G - 256) == SHAPE
+
+
+def test_gradients_of_a_backward_call_must_be_apart(lib):
+    """dA and dB are written by one launch.  The other refusals keep their order: these calls have everything else right, and none is launched."""
+    from paper_2510_11696_amd.binding import _BackwardDesc
+    G, M, K, N, r = 0x100000, 4, 64, 32, 8
+    size_a, size_b = 4 * r * K, 4 * r * N
+
+    def single(dA, dB):
+        return lib.nvfp4_lora_linear_backward(FAKE, FAKE, M, K, N, K, N, FAKE, FAKE, FAKE, FAKE, r, 1.0, FAKE, K, dA, dB, FAKE, BIG, None)
+
+    def group(*grads):
+        d = (_BackwardDesc * len(grads))()
+        for m, g in zip(d, grads):
+            m.dy, m.lddy, m.N, m.packed_t, m.tensor_scale = FAKE, N, N, FAKE, FAKE
+            if g is not None:
+                m.A, m.B, m.r, m.lora_scale, m.dA, m.dB = FAKE, FAKE, r, 1.0, *g
+        return lib.nvfp4_lora_linear_backward_group(FAKE, M, K, K, ctypes.cast(d, p), len(grads), FAKE, K, FAKE, BIG, None)
+    for call in (single, lambda *g: group(g), lambda *g: group(None, g), lambda *g: group((8 * G, 9 * G), g)):
+        for dA, dB in ((G, G), (G, G + size_a - 4), (G + size_b - 4, G)):
+            assert call(dA, dB) == SHAPE, (dA, dB)
+    ok = (G, 2 * G)
+    for bad in (ok, (G + size_a - 4, 3 * G), (3 * G, G + size_a - 4), (2 * G, 3 * G), (3 * G, 2 * G - size_b + 4), (3 * G, 2 * G)):
+        assert group(ok, bad) == SHAPE and group(ok, None, bad) == SHAPE and group(bad, None, (5 * G, 6 * G), ok) == SHAPE, bad

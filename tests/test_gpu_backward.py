@@ -298,3 +298,54 @@ def test_down_projection_of_one_adapter_is_as_exact_as_many_short_chains(M, K):
     err, bound = (float((t.double() - want).norm() / want.norm()) for t in (dB, total))
     print(err / bound)
     assert err <= 1.05 * bound, (M, K, err, bound)
+
+
+def test_gradients_written_where_the_caller_says():
+    """A group's gradients in given buffers, in new ones, or member by member in either: the same bits, nothing beside them written; gradients
+    of one call on shared memory are refused."""
+    M, K, Ns, rs = 70, 320, (160, 96, 96), (16, 8, 0)
+    x = qs.activations(M, K, 9500).cuda()
+    dys = [qs.activations(M, N, 9510 + i, std=0.5).cuda() for i, N in enumerate(Ns)]
+    weights = [qerl.nvfp4_prepack_t(*qerl.nvfp4_quantize(torch.from_numpy(cases.gaussian(N, K, 9520 + i)).to(torch.bfloat16).cuda()))
+               for i, N in enumerate(Ns)]
+    As, Bs = zip(*([t.cuda() for t in qs.lora_pair(N, K, r, 9530 + i, b_std=0.05)] if r else (None, None) for i, (N, r) in enumerate(zip(Ns, rs))))
+    call = lambda **kw: qerl.nvfp4_lora_linear_backward_group(x, dys, weights, As, Bs, [1.5] * 3, **kw)
+    dx, want = call()
+
+    def buffer(*shape):
+        flat = torch.full((shape[0] * shape[1] + 32,), float("nan"), device="cuda")
+        return flat, flat[16:-16].view(shape)
+    for given in ((True, True, True, True), (True, False, False, True), (False, True, True, False)):
+        flats, places = [], []
+        for i in range(2):
+            for j, shape in enumerate(((rs[i], K), (Ns[i], rs[i]))):
+                flat, place = buffer(*shape) if given[2 * i + j] else (None, None)
+                flats.append(flat)
+                places.append(place)
+        dAs, dBs = [places[0], places[2], None], [places[1], places[3], None]
+        got_dx, got = call(dAs=dAs, dBs=dBs)
+        assert torch.equal(got_dx, dx) and got[2] == (None, None)
+        for i in range(2):
+            for j, t in enumerate(got[i]):
+                assert torch.equal(t, want[i][j]), (given, i, j)
+                if given[2 * i + j]:
+                    flat = flats[2 * i + j]
+                    assert t.data_ptr() == flat[16:].data_ptr() and bool(torch.isnan(flat[:16]).all()) and bool(torch.isnan(flat[-16:]).all())
+    one_dx, dA, dB = qerl.nvfp4_lora_linear_backward(x, dys[0], weights[0], As[0], Bs[0], 1.5, dA=torch.empty_like(want[0][0]))
+    assert torch.equal(dA, want[0][0]) and dB.shape == (Ns[0], rs[0])
+    # shared memory
+    shared = torch.zeros((max(Ns) * 16 + 16 * K,), device="cuda")
+    at = lambda start, *shape: shared[start:start + shape[0] * shape[1]].view(shape)
+    for kw in (dict(dAs=[at(0, 16, K), at(16 * K - 4, 8, K), None]), dict(dAs=[at(0, 16, K), None, None], dBs=[at(100, 160, 16), None, None]),
+               dict(dBs=[at(0, 160, 16), at(0, 96, 8), None]), dict(dAs=[None, at(0, 8, K), None], dBs=[at(0, 160, 16), None, None])):
+        with pytest.raises(qerl.QerlError):
+            call(**kw)
+    with pytest.raises(qerl.QerlError):
+        qerl.nvfp4_lora_linear_backward(x, dys[0], weights[0], As[0], Bs[0], 1.5, dA=at(0, 16, K), dB=at(0, 160, 16))
+    assert not bool(shared.any())
+    for kw in (dict(dAs=[None, None]), dict(dAs=[torch.empty((16, K + 1), device="cuda"), None, None]), dict(dBs=[None, None, torch.empty((96, 8), device="cuda")]),
+               dict(dAs=[torch.empty((K, 16), device="cuda").t(), None, None])):
+        with pytest.raises(ValueError):
+            call(**kw)
+    with pytest.raises(TypeError):
+        call(dAs=[torch.empty((16, K), dtype=torch.bfloat16, device="cuda"), None, None])
