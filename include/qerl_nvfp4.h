@@ -326,6 +326,7 @@ QERL_API int nvfp4_lora_linear_packed_swiglu(const void* gate_bf16, const void* 
  *   r == 0: only dX is written (x, A, B, dA, dB may be NULL).
  *   workspace: >= nvfp4_lora_linear_backward_workspace_bytes(M, N, K, r),
  *   256-byte aligned; needs no initialisation.
+ * M == 0 is a no-op: dA and dB, whose sums have no terms then, are left as they are.
  * Errors: as the forward functions; QERL_ERR_SHAPE for dA and dB that share memory.
  */
 QERL_API size_t nvfp4_prepack_t_bytes(int64_t N, int64_t K);   /* host */

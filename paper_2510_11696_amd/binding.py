@@ -445,7 +445,7 @@ def nvfp4_lora_linear_backward(x, dy, w: PackedWeightT, A: Optional[torch.Tensor
                                workspace: Optional[torch.Tensor] = None, dA: Optional[torch.Tensor] = None,
                                dB: Optional[torch.Tensor] = None):
     """(dx bf16 [M, K], dA fp32 [r, K] or None, dB fp32 [N, r] or None).  dA, dB: where to write the gradients (an optimizer's
-    buffers), or None for new tensors."""
+    buffers), or None for new tensors; without rows they are zero."""
     lib = load_library()
     M, N, lddy = _rows(dy, "dy")
     K = w.K
@@ -465,6 +465,9 @@ def nvfp4_lora_linear_backward(x, dy, w: PackedWeightT, A: Optional[torch.Tensor
         a_ptr, b_ptr = _dev(A, torch.bfloat16, "A"), _dev(B, torch.bfloat16, "B")
         dA, dB = _grad_buffer(dA, (r, K), dy.device, "dA"), _grad_buffer(dB, (N, r), dy.device, "dB")
         da_ptr, db_ptr = _dev(dA, torch.float32, "dA"), _dev(dB, torch.float32, "dB")
+        if M == 0:
+            dA.zero_()
+            dB.zero_()
     elif dA is not None or dB is not None:
         raise ValueError("dA and dB belong to an adapter")
     dx = torch.empty((M, K), dtype=torch.bfloat16, device=dy.device)
@@ -489,7 +492,7 @@ class _BackwardDesc(ctypes.Structure):
 def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_scales=None, workspace: Optional[torch.Tensor] = None,
                                      dAs=None, dBs=None):
     """Backward of several linears that read the same x: (dx bf16 [M, K] summed over the members, [(dA_i, dB_i)]).  dAs, dBs: lists of
-    tensors (or None) to write the gradients to."""
+    tensors (or None) to write the gradients to; without rows they are zero."""
     lib = load_library()
     n = len(weights)
     As = As if As is not None else [None] * n
@@ -517,6 +520,9 @@ def nvfp4_lora_linear_backward_group(x, dys, weights, As=None, Bs=None, lora_sca
             dB = _grad_buffer(dBs[i] if dBs is not None else None, (N, r), x.device, "dB")
             d.A, d.B, d.r, d.lora_scale = _dev(A, torch.bfloat16, "A"), _dev(B, torch.bfloat16, "B"), r, float(lora_scales[i])
             d.dA, d.dB = _dev(dA, torch.float32, "dA"), _dev(dB, torch.float32, "dB")
+            if M == 0:
+                dA.zero_()
+                dB.zero_()
         elif any(v is not None and v[i] is not None for v in (dAs, dBs)):
             raise ValueError("dA and dB belong to an adapter")
         grads.append((dA, dB))

@@ -349,3 +349,19 @@ def test_gradients_written_where_the_caller_says():
             call(**kw)
     with pytest.raises(TypeError):
         call(dAs=[torch.empty((16, K), dtype=torch.bfloat16, device="cuda"), None, None])
+
+
+def test_a_call_without_rows_leaves_no_gradient_of_the_last_one():
+    """Sums over no rows: zeros in the caller's buffers and in new ones."""
+    K, N, r = 64, 96, 8
+    w = qerl.nvfp4_prepack_t(*qerl.nvfp4_quantize(torch.from_numpy(cases.gaussian(N, K, 9600)).to(torch.bfloat16).cuda()))
+    A, B = (t.cuda() for t in qs.lora_pair(N, K, r, 9601))
+    x, dy = torch.empty((0, K), dtype=torch.bfloat16, device="cuda"), torch.empty((0, N), dtype=torch.bfloat16, device="cuda")
+    full = lambda *s: torch.full(s, 7.0, device="cuda")
+    for given in (True, False):
+        dA, dB = (full(r, K), full(N, r)) if given else (None, None)
+        dx, gA, gB = qerl.nvfp4_lora_linear_backward(x, dy, w, A, B, 1.0, dA=dA, dB=dB)
+        assert dx.shape == (0, K) and not bool(gA.any()) and not bool(gB.any()) and (not given or gA.data_ptr() == dA.data_ptr())
+        dA, dB = (full(r, K), full(N, r)) if given else (None, None)
+        dx, grads = qerl.nvfp4_lora_linear_backward_group(x, [dy, dy], [w, w], [A, None], [B, None], [1.0, 0.0], dAs=[dA, None], dBs=[dB, None])
+        assert dx.shape == (0, K) and not bool(grads[0][0].any()) and not bool(grads[0][1].any()) and grads[1] == (None, None)
