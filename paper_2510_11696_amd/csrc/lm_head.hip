@@ -444,7 +444,7 @@ extern "C" int lm_head_prepack_t(const void* W, int64_t V, int64_t H, int64_t ld
 }
 
 extern "C" size_t lm_head_logprob_workspace_bytes(int64_t M, int64_t V, int64_t H, int gradient) {
-  if (M < 0 || V < 1 || H < 8 || M > 0x7fffffff || V > kMaxVocab || H >= kMaxLd) return 0;
+  if (M < 0 || V < 1 || H < 8 || H % 8 != 0 || M > 0x7fffffff || V > kMaxVocab || H >= kMaxLd) return 0;
   size_t most = 256;                             // a smaller call may split its sums further: the largest over all token blocks
   for (int64_t m : {(int64_t)32, (int64_t)64, (int64_t)128}) {
     const size_t b = M > 0 ? plan_head(M < m ? M : m, V, H, gradient != 0).bytes : 0;

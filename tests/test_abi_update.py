@@ -231,3 +231,16 @@ def test_gradients_of_a_backward_call_must_be_apart(lib):
     ok = (G, 2 * G)
     for bad in (ok, (G + size_a - 4, 3 * G), (3 * G, G + size_a - 4), (2 * G, 3 * G), (3 * G, 2 * G - size_b + 4), (3 * G, 2 * G)):
         assert group(ok, bad) == SHAPE and group(ok, None, bad) == SHAPE and group(bad, None, (5 * G, 6 * G), ok) == SHAPE, bad
+
+
+def test_logprob_workspace_is_0_for_every_size_that_is_refused(lib):
+    size = lib.lm_head_logprob_workspace_bytes
+    for g in (0, 1):
+        for M, V, H in ((4, 100, 9), (4, 100, 60), (4, 100, 4), (4, 100, 0), (4, 100, 1 << 18), (-1, 100, 64), (1 << 31, 100, 64), (4, 0, 64), (4, (1 << 22) + 1, 64)):
+            assert size(M, V, H, g) == 0, (M, V, H)
+            if M > 0:
+                assert _logprob(lib, bool(g), M=M, V=V, H=H, ldx=1 << 18 if H >= 1 << 18 else 64, ldw=1 << 18 if H >= 1 << 18 else 64) == SHAPE, (M, V, H)
+        for M, V, H in ((4, 100, 8), (4, 100, (1 << 18) - 8), (1, 1 << 22, 64)):
+            assert size(M, V, H, g) > 0, (M, V, H)
+    with pytest.raises(ValueError):
+        qerl.lm_head_workspace(4, 100, 60)
