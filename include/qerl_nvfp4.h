@@ -584,7 +584,8 @@ QERL_API int lm_head_logprob_backward(const float* grad_logprob_f32, const float
  *   block with an infinity or a NaN, which reads as NaN throughout).  A byte of m is sign, 4 exponent and 3 mantissa bits e, q
  *   with the value (8 + q) 2^(e - 14 - 3) 2^(f - 127) (e = 0: q 2^(1 - 14 - 3) 2^(f - 127)); a byte of v 5 and 3 bits, 30 in
  *   place of 14, and never 0 for a v above zero.  Both are rounded up in magnitude with the probability of what is cut off
- *   (to nearest, 0.1 and 0.001 of a moment would not move it), by 16 random bits per element:
+ *   (to nearest, 0.1 and 0.001 of a moment would not move it; a value that would round up to 2^128 stays at 1.875 2^127), by 16 random
+ *   bits per element:
  *   Philox4x32 with 10 rounds, counter (b lo, b hi, t lo, t hi), key (seed lo, seed hi), b the group of eight state elements,
  *   element j of it the low (even j) or high half of word j / 2.  Zero-filled memory is the state before the first step.
  *   Its memory must be apart from the tensors' and the table's: lora_adamw_check_state says whether a state fits a list of tensors and (if not

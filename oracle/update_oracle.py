@@ -73,7 +73,7 @@ def decode(codes, field, exponent_bits):
 
 def _encode(x, fractions, exponent_bits):
     """(codes of the magnitudes, field): rounded up where the distance from the value below, in steps, plus the fraction (a multiple of 2^-16)
-    reaches 1.  Distances are taken to 20 bits of a step, as an fp32 near the bottom of its range holds them (only magnitudes below the
+    reaches 1; where that would be 2^128, the value below stays.  Distances are taken to 20 bits of a step, as an fp32 near the bottom of its range holds them (only magnitudes below the
     format's smallest normal value have more)."""
     x = np.asarray(x, np.float32)
     field = block_field(x)
@@ -82,7 +82,9 @@ def _encode(x, fractions, exponent_bits):
     lo = np.clip(np.searchsorted(grid, q, side="right") - 1, 0, len(grid) - 2)
     part = (q - grid[lo]) / (grid[lo + 1] - grid[lo])
     part = np.rint(part * 2.0 ** 20) / 2.0 ** 20
-    return lo + (part + np.asarray(fractions).reshape(-1, BLOCK) >= 1.0), field
+    code = lo + (part + np.asarray(fractions).reshape(-1, BLOCK) >= 1.0)
+    top = 14 if exponent_bits == 4 else 30
+    return np.where(field[:, None] == 254, np.minimum(code, 8 * top + 7), code), field
 
 
 def encode_first(x, fractions):

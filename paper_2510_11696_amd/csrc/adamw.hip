@@ -9,8 +9,8 @@
 // 255 for a block with an infinity or a NaN, which reads as NaN throughout).  Powers of two scale exactly, so nothing is lost but the
 // 8-bit rounding itself.
 //   m: sign, 4 exponent bits, 3 mantissa bits (value: the bits at fp32's bit 20, times 2^(f - 14)).  The largest magnitude of a block has
-//      exponent 14 of 15, so rounding up never overflows.
-//   v: 5 exponent bits, 3 mantissa bits, times 2^(f - 30).  A v above zero never becomes zero (smallest code 1): m reaches down to 2^-16 of
+//      exponent 14 of 15, so rounding up never overflows the code; where the value would be 2^128 (f = 254), 1.875 2^127 stands in its place.
+//   v: 5 exponent bits, 3 mantissa bits, times 2^(f - 30), 30 of 31 as above.  A v above zero never becomes zero (smallest code 1): m reaches down to 2^-16 of
 //      its block's largest, sqrt(v) to 2^-16 too, and m / sqrt(v) stays bounded.
 // Both are rounded up in magnitude with the probability of what is cut off.  To nearest, they would stop moving: under a steady gradient
 // g the first moment changes by 0.1 (g - m) and stays where that is under half a step, up to a quarter below g; the second by
@@ -84,14 +84,16 @@ __device__ __forceinline__ float decode_m(uint32_t c, uint32_t field) {
 __device__ __forceinline__ float decode_v(uint32_t c, uint32_t field) {
   return field == 255u ? __uint_as_float(0x7fc00000u) : ldexpf(__uint_as_float(c << 20), (int)field - 30);
 }
+// largest code: the next one's value is not finite where the block reaches fp32's last power of two
+__device__ __forceinline__ uint32_t last_code(int top, uint32_t field) { return field == 254u ? 8u * top + 7u : 8u * top + 8u; }
 __device__ __forceinline__ uint32_t encode_m(float x, uint32_t field, uint32_t random16) {
   const uint32_t b = __float_as_uint(ldexpf(fabsf(x), 14 - (int)field));
-  const uint32_t c = (b + (random16 << 4)) >> 20;
+  const uint32_t up = (b + (random16 << 4)) >> 20, last = last_code(14, field), c = up < last ? up : last;
   return field == 255u ? 0u : c | (x < 0.f ? 128u : 0u);
 }
 __device__ __forceinline__ uint32_t encode_v(float x, uint32_t field, uint32_t random16) {
   const uint32_t b = __float_as_uint(ldexpf(x, 30 - (int)field));
-  const uint32_t c = (b + (random16 << 4)) >> 20;
+  const uint32_t up = (b + (random16 << 4)) >> 20, last = last_code(30, field), c = up < last ? up : last;
   return field == 255u || !(x > 0.f) ? 0u : c > 1u ? c : 1u;
 }
 

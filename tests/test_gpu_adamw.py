@@ -361,3 +361,26 @@ def test_a_state_on_memory_of_the_tensors_is_refused():
     plan = qerl.lora_adamw_plan([p], [g], [c], state_bits=32, state=(cut(128, 64), cut(192, 64)))
     qerl.lora_adamw_step(plan, lr=1e-3, step=1)
     assert bool((flat[:64] < 0).all()) and bool((flat[128:256] > 0).all()) and not bool(flat[256:].any())
+
+
+def test_moments_in_8_bits_at_the_end_of_the_range_stay_finite():
+    """Moments between 1.875 2^127 and 2^128, over seeds that round most of them up: with beta2 = 0 the second is g^2, with beta1 = 0 the first g."""
+    h = dict(lr=0.0, eps=1e-8, weight_decay=0.0, step=1)
+    edge = np.float32(1.875 * 2.0 ** 127)
+    for seed in range(3):
+        s = _Set([256], 8, 9)
+        s.g = [np.sqrt(np.linspace(0.90, 0.9999, 256) * np.float64(np.finfo(np.float32).max)).astype(np.float32) * (np.arange(256) % 2 * 2 - 1).astype(np.float32)]
+        s.gg[0].copy_(torch.from_numpy(s.g[0]))
+        b = dict(h, beta1=0.9, beta2=0.0, seed=seed)
+        qerl.lora_adamw_step(s.plan, **b)
+        s.reference(**b)
+        s.check()
+        assert s.v.max() == edge and (s.v == edge).sum() > 100
+        # the first (g^2 is infinite then, so the second and the parameters are not of this world)
+        s = _Set([256], 8, 9, copies=False)
+        g = (np.linspace(1.75, 1.99, 256) * 2.0 ** 127).astype(np.float32) * (np.arange(256) % 2 * 2 - 1).astype(np.float32)
+        s.gg[0].copy_(torch.from_numpy(g))
+        qerl.lora_adamw_step(s.plan, beta1=0.0, beta2=0.9, seed=seed, **h)
+        want = uo.decode(*uo.encode_first(g, uo.random_fractions(256, 1, seed)), 4)
+        got = qerl.lora_adamw_moments(s.plan)[0].cpu().numpy()
+        assert np.array_equal(got, want) and np.abs(got).max() == edge

@@ -76,3 +76,17 @@ def test_adamw_first_step_moves_by_the_rate():
     assert np.allclose(p, -1e-3 * np.sign(g), rtol=2e-4)
     p2, _, _ = uo.adamw(np.ones(3), g * 4, np.zeros(3), np.zeros(3), 1e-3, 0.9, 0.999, 1e-8, 0.1, 1, grad_scale=0.25)
     assert np.allclose(p2, 1 - 1e-4 - 1e-3 * np.sign(g), rtol=1e-6)
+
+
+def test_the_largest_values_stay_finite():
+    x = np.full(32, np.finfo(np.float32).max, np.float32)
+    x[1::2] = 1.875 * 2.0 ** 127
+    for u in (0.0, 0.5, 1 - 2.0 ** -16):
+        for sign in (1, -1):
+            codes, field = uo.encode_first(sign * x, np.full(32, u))
+            assert np.all(field == 254) and np.array_equal(uo.decode(codes, field, 4), np.full(32, sign * 1.875 * 2.0 ** 127, np.float32))
+        codes, field = uo.encode_second(x, np.full(32, u))
+        assert np.all(field == 254) and np.array_equal(uo.decode(codes, field, 5), np.full(32, 1.875 * 2.0 ** 127, np.float32))
+    # one power of two lower the next value exists, and is reached
+    codes, field = uo.encode_first(x / 2, np.full(32, 1 - 2.0 ** -16))
+    assert np.all(field == 253) and np.array_equal(uo.decode(codes, field, 4)[:2], [2.0 ** 127, 1.875 * 2.0 ** 126])
