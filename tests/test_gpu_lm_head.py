@@ -443,3 +443,19 @@ def test_a_large_probability_beside_a_token_that_is_nearly_certain():
     got = qerl.lm_head_logprob_grad(x, qerl.lm_head_prepack(W), t.cuda())
     assert float(got[0].median()) > -1e-3
     _check_slope(got[3], x, W, t.numpy(), 1.0, "sure")
+
+
+@pytest.mark.parametrize("m", [20, 50, 100, 200, 300])
+def test_rows_beside_one_that_is_not_finite_are_as_without_it(m):
+    """Both calls on every tile for few and for many rows, against the same call on clean rows, bit for bit."""
+    V, H = 500, 64
+    x, W, t = _inputs(m, V, H, 12)
+    head, td = qerl.lm_head_prepack(W), t.cuda()
+    calls = (lambda: qerl.lm_head_logprob(x, head, td, entropy=True), lambda: qerl.lm_head_logprob_grad(x, head, td, entropy=True))
+    clean = [call() for call in calls]
+    x[3, 5], x[7, 1], x[m - 1, 63] = float("nan"), float("inf"), -float("inf")
+    rest = [i for i in range(m) if i not in (3, 7, m - 1)]
+    for call, good in zip(calls, clean):
+        for a, b in zip(call(), good):
+            assert torch.equal(a[rest], b[rest])
+            assert not bool(torch.isfinite(a[3]).any())
