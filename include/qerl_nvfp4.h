@@ -598,7 +598,7 @@ QERL_API int lm_head_logprob_backward(const float* grad_logprob_f32, const float
  *   *scale = min(1, max_norm / (norm + 1e-6)), NaN if the norm is not finite: pass it as grad_scale.  norm may be NULL.
  *   The sums of its workgroups pass through the table, so norms of one plan must be ordered on one stream, as its steps must.
  * lora_adamw_moments: the values of an 8-bit state as fp32, m and v [state elements] (inspection, checkpoints).
- * Errors: NULL pointers (copy_bf16 may be NULL); n < 0, n_tensors outside 1..2^20, more than 2^31 - 1 pieces of 2048
+ * Errors: NULL pointers (copy_bf16 may be NULL); n < 0, n_tensors outside 1..2^20, more than 2^24 - 1 pieces of 2048
  * elements, memory that a step writes named twice (tensors, table or, where they are checked, parts of the state), bits other than 8 and 32, step < 1, lr, weight_decay < 0 or not
  * finite, betas outside [0, 1), eps that is 0 or less or not finite, eps and factors (1 - lr wd, lr / (1 - b1^t)) as fp32 (QERL_ERR_SHAPE); parameters, gradients, copies, m or v not 16-byte aligned
  * (QERL_ERR_ALIGN); table too small or misaligned (QERL_ERR_WORKSPACE).

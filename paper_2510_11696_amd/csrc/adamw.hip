@@ -32,6 +32,7 @@ namespace qerl {
 constexpr int kStateBlock = 32;       // elements that share a scale byte; tensors start at multiples of it in the state
 constexpr int kChunk = 2048;          // elements of one tensor that a workgroup takes at a time
 constexpr int kAdamThreads = 256;
+constexpr int64_t kMaxChunks = ((int64_t)1 << 24) - 1;   // a launch has fewer than 2^32 threads
 
 struct AdamTensor { float* p; uint16_t* copy; const float* g; int64_t n, state0, chunk0; };   // state0: first element in the state
 constexpr int kTableBatch = 64;
@@ -335,7 +336,7 @@ static bool adam_layout(const qerl_adamw_tensor* t, int n, AdamLayout& l) {
     if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return false;
     l.elements += ceil_div(t[i].n, kStateBlock) * kStateBlock;
     l.chunks += ceil_div(t[i].n, kChunk);
-    if (l.chunks > 0x7fffffff) return false;
+    if (l.chunks > kMaxChunks) return false;
   }
   l.bytes = (owner_offset(n) + (size_t)l.chunks * 4 + 255) & ~(size_t)255;
   return true;
@@ -346,7 +347,7 @@ static const uint32_t* owner_of(const qerl_adamw_plan* p) {
 }
 static int plan_status(const qerl_adamw_plan* p) {
   if (!p) return QERL_ERR_NULL;
-  if (p->chunks < 0 || p->chunks > 0x7fffffff || p->n_tensors < 1 || p->elements < 0) return QERL_ERR_SHAPE;
+  if (p->chunks < 0 || p->chunks > kMaxChunks || p->n_tensors < 1 || p->elements < 0) return QERL_ERR_SHAPE;
   return p->table ? QERL_OK : QERL_ERR_NULL;
 }
 

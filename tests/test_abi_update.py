@@ -244,3 +244,15 @@ def test_logprob_workspace_is_0_for_every_size_that_is_refused(lib):
             assert size(M, V, H, g) > 0, (M, V, H)
     with pytest.raises(ValueError):
         qerl.lm_head_workspace(4, 100, 60)
+
+
+def test_adamw_pieces_that_one_launch_has_no_threads_for(lib):
+    """A workgroup of 256 threads per piece of 2048 elements, fewer than 2^32 threads in a launch."""
+    most = 2048 * (2 ** 24 - 1)
+    one = lambda *ns: ctypes.cast(_tensors([(FAKE, None, FAKE, n) for n in ns]), p)
+    assert lib.lora_adamw_state_elements(one(most), 1) == most and lib.lora_adamw_plan_bytes(one(most), 1) > 4 * (2 ** 24 - 1)
+    for ns in ((most + 1,), (most, 1), (most // 2, most // 2, 4096)):
+        assert lib.lora_adamw_state_elements(one(*ns), len(ns)) == -1 and lib.lora_adamw_plan_bytes(one(*ns), len(ns)) == 0, ns
+    assert lib.lora_adamw_state_elements(one(most - 2048, 1, 0), 3) == most - 2048 + 32
+    st, h = _AdamWState(8, FAKE, FAKE, FAKE, FAKE), _AdamWHyper(1e-3, 0.9, 0.999, 1e-8, 0.0, 1)
+    assert lib.lora_adamw_step(ctypes.byref(_AdamWPlanStruct(FAKE, most + 2048, 2 ** 24, 1)), ctypes.byref(st), ctypes.byref(h), None) == SHAPE
