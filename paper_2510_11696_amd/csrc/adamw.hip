@@ -232,7 +232,8 @@ __global__ __launch_bounds__(256) void adamw_moments_kernel(const uint8_t* mc, c
 
 // Sum of squares of all gradients: a workgroup sums a contiguous range of chunks in fp64 (a square of an fp32 value is exact there); the
 // last one to finish adds the workgroups' sums in their order, so that nothing depends on which one it was, and sets the counter back.
-// Sums and counter pass between the XCDs' caches by accesses at device scope.
+// Sums and counter pass between the XCDs' caches by accesses at device scope.  323 MB in 100 us (3.2 TB/s): a group of chunks waits for its tensors'
+// numbers, then for their table entries, then for its gradients, before the next one begins.
 constexpr int kNormGroups = 2048, kNormAhead = 4;
 struct NormArea { double partial[kNormGroups]; uint32_t arrived; };
 __device__ __forceinline__ double block_sum64(double v, double* smem) {

@@ -564,7 +564,7 @@ using Head64 = HeadCfg<2, 2, 2, 1, 3, 3>;        // 128 rows x 64 tokens
 using Head128 = HeadCfg<2, 2, 4, 2, 3, 2>;       // 256 rows x 128 tokens
 using Head256 = HeadCfg<4, 2, 2, 4, 3, 2>;       // 256 rows x 256 tokens
 using HeadHalf = HeadCfg<2, 2, 2, 4, 3, 2>;      // 128 rows x 256 tokens
-using Head320 = HeadCfg<5, 2, 2, 4, 2, 2>;       // 320 rows x 256 tokens: sums whose tiles of 256 would leave a round of workgroups half empty
+using Head320 = HeadCfg<5, 2, 2, 4, 2, 2>;       // 320 rows x 256 tokens (six registers in scratch): sums whose tiles of 256 would leave a round of workgroups half empty
 
 // The smallest tile that holds all tokens, so that few tokens stream the weights through small workgroups; beyond 128 tokens 256 rows, or 128
 // where those would leave half of the compute units without a tile (200 rows of 32001 x 1024: 35 -> 25 us).
