@@ -459,3 +459,41 @@ def test_rows_beside_one_that_is_not_finite_are_as_without_it(m):
         for a, b in zip(call(), good):
             assert torch.equal(a[rest], b[rest])
             assert not bool(torch.isfinite(a[3]).any())
+
+
+@pytest.mark.parametrize("M,V", [(300, 4099), (2100, 60000)])
+def test_large_probabilities_in_a_used_workspace_and_on_replay(M, V):
+    """One and several pieces: the same bits whatever the workspace holds, again, and on every replay with other rows, some of them with a large
+    probability, some without, some without a loss."""
+    H = 64
+    x, W, t = _inputs(M, V, H, 900 + M, sure=0.0)
+    head, g = qerl.lm_head_prepack(W), torch.Generator().manual_seed(M)
+    Wf = W.float().cpu()
+
+    def rows(i):
+        u, z = torch.randint(0, V, (M,), generator=g), torch.tensor([0.0, 9.0, 13.0])[torch.randint(0, 3, (M,), generator=g)][:, None]
+        w = Wf[u]
+        x.copy_((torch.randn((M, H), generator=g) * 0.5 + z * w / (w * w).sum(1, keepdim=True)).to(torch.bfloat16))
+        td.copy_(torch.where(torch.rand((M,), generator=g) < 0.2 * i, torch.full_like(t, -1), t))
+    td = t.cuda()
+    rows(1)
+    ws = qerl.lm_head_workspace(M, V, H)
+    out = [torch.empty((M,), device="cuda") for _ in range(3)] + [torch.empty((M, H), device="cuda")]
+    call = lambda: qerl.lm_head_logprob_grad(x, head, td, entropy=True, workspace=ws, out=out)
+    for byte in (0, 255, 0x7F):
+        ws.fill_(byte)
+        call()
+        first = [o.clone() for o in out] if byte == 0 else first
+        assert all(torch.equal(a, b) for a, b in zip(first, out)), byte
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        rows(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in out]
+        assert all(torch.equal(a, b) for a, b in zip(got, qerl.lm_head_logprob_grad(x, head, td, entropy=True)))
+        keep = torch.nonzero(td.cpu() >= 0)[:200, 0]
+        _check_slope(got[3][keep.cuda()], x[keep.cuda()], W, t.numpy()[keep.numpy()], 1.0, (M, V, i))
