@@ -88,50 +88,65 @@ __global__ __launch_bounds__(256) void head_first_ref_kernel(const HeadArgs a, f
 // by up to 2^-8 of itself, as much as dx by its own rounding.  So all that hold kLargeShare of what all others hold together, 32 at most, are looked
 // up again where the parts' largest logits say that there are some: the logit formed once more in fp32, and what the rounding cut off kept for the
 // slope.  The rest is off by 2^-8 / sqrt(32) of the slope at most, in the root mean square.  Measured on rows whose mass one or five other tokens
-// share, slope against 64 bits: 9e-4 of itself without, 2e-6 and 2e-5 with; time for 4096 rows of 152064 x 5120 10.17 ms without, 10.21 with where no
-// probability is large, 10.32 and 10.48 with one and five per row; 200 rows of 32001 x 1024 74 us, 76, 78 and 84.
-// Of a piece, by a workgroup for its token: those of at least `least` (relative to ref); lane i of the first wave holds slot i in `mine`.
-// Where the slots do not suffice (earlier pieces' sums were smaller) the largest stay.
+// share, slope against 64 bits: 9e-4 of itself without, 2e-6 and 2e-5 with; time for 4096 rows of 152064 x 5120 9.95 ms without, 10.00 with where no
+// probability is large, 10.10 and 10.23 with one and five per row; 200 rows of 32001 x 1024 74 us, 76, 80 and 83.
+// Of a piece, by a workgroup for its token: those of at least `least` (relative to ref), 33 at most as it is a share of their sum; lane i of the first
+// wave holds slot i in `mine`.  The first wave lists them, all four form their logits (five of them, 64 rows of 32000 x 2048: by one wave 98 us, 95),
+// and the first takes them up: where the slots do not suffice (earlier pieces' sums were smaller) the largest stay.
 constexpr int kLargeWords = (int)(((int64_t)1 << 22) / 64 / 64);   // a bit for each part of the largest vocabulary
-__device__ __forceinline__ void collect_large(const HeadArgs& a, const HeadLargeArgs& g, int token, int64_t row, float ref, float least, uint64_t* marks,
+struct LargeShared { uint64_t marks[kLargeWords]; int64_t at[kLargeSlots]; float kept[kLargeSlots], s[kLargeSlots]; int n; };
+__device__ __forceinline__ void collect_large(const HeadArgs& a, const HeadLargeArgs& g, int token, int64_t row, float ref, float least, LargeShared& sh,
                                               HeadLarge& mine, int& count) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const HeadPart* part = a.part + (int64_t)token * a.part_ld + a.part0;
   for (int b0 = 0; b0 < g.parts; b0 += 256) {
     const int b = b0 + threadIdx.x;
     const uint64_t votes = __ballot(b < g.parts && exp2_fast(part[b < g.parts ? b : 0].top - ref) >= least);
-    if (lane == 0) marks[b0 / 64 + wave] = votes;
+    if (lane == 0) sh.marks[b0 / 64 + wave] = votes;
   }
   __syncthreads();
-  if (wave != 0) return;
-  const uint16_t* x = a.b + row * a.ldb;
-  const uint16_t* p = a.p + (int64_t)token * a.ldp;
-  const int words = (g.parts + 63) / 64;
-  for (int w0 = 0; w0 < words; w0 += 64) {
-    const uint64_t word = w0 + lane < words ? marks[w0 + lane] : 0;
-    for (uint64_t some = __ballot(word != 0); some; some &= some - 1) {
-      const int from = __ffsll((unsigned long long)some) - 1;
-      for (uint64_t bits = __shfl((unsigned long long)word, from, 64); bits; bits &= bits - 1) {
-        const int64_t r0 = ((int64_t)(w0 + from) * 64 + __ffsll((unsigned long long)bits) - 1) * g.part_rows;
-        for (int64_t r = r0; r < r0 + g.part_rows; r += 64) {
-          const float value = r + lane < a.rows ? bf16_bits_to_f32(p[r + lane]) : 0.f;
-          for (uint64_t hits = __ballot(value >= least); hits; hits &= hits - 1) {
-            const int at = __ffsll((unsigned long long)hits) - 1;
-            const float s = wave_logit(x, a.a + (r + at) * a.lda, a.k, lane) * a.scale, kept = __shfl(value, at, 64);
-            int slot = count;
-            if (count == kLargeSlots) {
-              float lowest = mine.s;
-#pragma unroll
-              for (int o = 32; o > 0; o >>= 1) lowest = fminf(lowest, __shfl_xor(lowest, o, 64));
-              slot = s > lowest ? __ffsll((unsigned long long)__ballot(mine.s == lowest)) - 1 : kLargeSlots;
-            } else {
-              ++count;
-            }
-            if (lane == slot) mine = HeadLarge{(int)(a.row0 + r + at), ref, exp2_fast(s - ref) - kept, s};
+  if (wave == 0) {
+    const uint16_t* p = a.p + (int64_t)token * a.ldp;
+    const int words = (g.parts + 63) / 64;
+    int n = 0;
+    for (int w0 = 0; w0 < words; w0 += 64) {
+      const uint64_t word = w0 + lane < words ? sh.marks[w0 + lane] : 0;
+      for (uint64_t some = __ballot(word != 0); some; some &= some - 1) {
+        const int from = __ffsll((unsigned long long)some) - 1;
+        for (uint64_t bits = __shfl((unsigned long long)word, from, 64); bits; bits &= bits - 1) {
+          const int64_t r0 = ((int64_t)(w0 + from) * 64 + __ffsll((unsigned long long)bits) - 1) * g.part_rows;
+          for (int64_t r = r0; r < r0 + g.part_rows; r += 64) {
+            const float value = r + lane < a.rows ? bf16_bits_to_f32(p[r + lane]) : 0.f;
+            const uint64_t hits = __ballot(value >= least);
+            const int to = n + __popcll(hits & (((uint64_t)1 << lane) - 1));
+            if (value >= least && to < kLargeSlots) { sh.at[to] = r + lane; sh.kept[to] = value; }
+            n += __popcll(hits);
           }
         }
       }
     }
+    if (lane == 0) sh.n = n < kLargeSlots ? n : kLargeSlots;
+  }
+  __syncthreads();
+  const int n = sh.n;
+  for (int i = wave; i < n; i += 4) {
+    const float s = wave_logit(a.b + row * a.ldb, a.a + sh.at[i] * a.lda, a.k, lane) * a.scale;
+    if (lane == 0) sh.s[i] = s;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  for (int i = 0; i < n; ++i) {
+    const float s = sh.s[i];
+    int slot = count;
+    if (count == kLargeSlots) {
+      float lowest = mine.s;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) lowest = fminf(lowest, __shfl_xor(lowest, o, 64));
+      slot = s > lowest ? __ffsll((unsigned long long)__ballot(mine.s == lowest)) - 1 : kLargeSlots;
+    } else {
+      ++count;
+    }
+    if (lane == slot) mine = HeadLarge{(int)(a.row0 + sh.at[i]), ref, exp2_fast(s - ref) - sh.kept[i], s};
   }
 }
 // least: the share of all that the others hold, a little less, so that roundings exclude nothing; NaN, which nothing reaches, where that is not finite
@@ -141,7 +156,7 @@ __device__ __forceinline__ float large_from(float others) {
 
 // Large probabilities of a piece that is not the last one (whose are looked up with the row results)
 __global__ __launch_bounds__(256) void head_large_kernel(const HeadArgs a, const HeadLargeArgs g) {
-  __shared__ uint64_t marks[kLargeWords];
+  __shared__ LargeShared large;
   __shared__ float sm[4];
   const int token = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (token >= head_tokens(a)) return;
@@ -159,7 +174,7 @@ __global__ __launch_bounds__(256) void head_large_kernel(const HeadArgs a, const
   HeadLarge* slot = g.slot + (int64_t)token * kLargeSlots;
   int count = g.first ? 0 : g.count[token];
   HeadLarge mine = lane < count ? slot[lane] : HeadLarge{0, 0.f, 0.f, kNegInf};
-  collect_large(a, g, token, row, ref, large_from(sum), marks, mine, count);
+  collect_large(a, g, token, row, ref, large_from(sum), large, mine, count);
   if (wave != 0) return;
   if (lane < count) slot[lane] = mine;
   if (lane == 0) {
@@ -175,7 +190,7 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int 
                                                           float* entropy, float* rest, float* e_scale, const HeadLargeArgs g, float* slope, int64_t ld_slope,
                                                           int64_t H) {
   __shared__ float sm[3][4];
-  __shared__ uint64_t marks[kLargeWords];
+  __shared__ LargeShared large;
   const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t target = a.targets[row];
   if (target < 0 || target >= a.V) {
@@ -246,7 +261,7 @@ __global__ __launch_bounds__(256) void head_finish_kernel(const HeadArgs a, int 
   HeadLarge* slot = g.slot + (int64_t)token * kLargeSlots;
   int count = g.first ? 0 : g.count[token];
   HeadLarge mine = lane < count ? slot[lane] : HeadLarge{0, 0.f, 0.f, kNegInf};
-  collect_large(a, g, token, row, ref, large_from(s * exp2_fast(base - ref)), marks, mine, count);
+  collect_large(a, g, token, row, ref, large_from(s * exp2_fast(base - ref)), large, mine, count);
   if (wave != 0) return;
   const bool stays = lane < count && exp2_fast(mine.s - base) >= large_from(s);   // what earlier pieces found may be small now
   const uint64_t all = __ballot(stays);
